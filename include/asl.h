@@ -67,7 +67,8 @@ typedef enum {
   ASL_ERR_WORKSPACE = -3,    /* workspace pointer null or too small                         */
   ASL_ERR_CUDA = -4,         /* a CUDA runtime/driver call failed                           */
   ASL_ERR_TIMEOUT = -5,      /* a bounded device-side wait gave up (see asl_device_status)  */
-  ASL_ERR_ARCH = -6          /* device is not sm_100: there is no fallback path             */
+  ASL_ERR_ARCH = -6,         /* device is not sm_100: there is no fallback path             */
+  ASL_ERR_PAGES = -7         /* the pool has too few free pages (see asl_pages_status)      */
 } asl_status;
 
 enum { ASL_POOL_AVG = 0, ASL_POOL_MAX = 1 };
@@ -336,6 +337,127 @@ asl_status asl_device_status(asl_ctx* ctx, void* stream, int32_t* where);
  * (barrier) or 92 (counter), and the query after that ASL_OK.  Needs a planned context; asynchronous
  * on `stream`. */
 asl_status asl_selftest_bounded_wait(asl_ctx* ctx, int32_t which, int64_t limit_ns, void* stream);
+
+/* ---- paged cache: where the kept rows go on living --------------------------------------------------------------
+ * Algorithm 1 returns a dense pruned cache.  What follows it (decoding, several samples or questions on one prompt,
+ * pruning once more) needs one that grows, is shared and is given back.  (The paper has no counterpart; its decoding
+ * appends to the pruned cache and attends over it.)
+ *
+ * A page holds page_size tokens of every kv head, in every layer: page p of layer l is k[l][p][H_k][page_size][d] (and
+ * v likewise).  A sequence lives in a slot: table[slot][j] is the page of its tokens [j * page_size, (j+1) * page_size),
+ * len[slot] its tokens (0: the slot is free), the same for all layers and heads; the kept lists of Algorithm 1 have one
+ * length for all heads, so row r of a kv head is the r-th token that this head kept.  refs[page] counts the slots that
+ * hold a page; 0 is free.  Table, len and refs belong to the calls below: zero them (and err) once, then only read
+ * them.  Entries of the table behind a slot's last page are meaningless.  Pages that several slots hold are full or
+ * are copied (the held tokens of them) by the asl_pages_reserve that grows one of those slots.
+ *
+ * The calls are asynchronous on `stream` like all others; those on one cache have to be ordered one behind another
+ * (one stream, or events), but for asl_attend calls, which only read it.  Slots and page numbers are checked on the
+ * device: what does not fit is left out (nothing is read or written out of bounds) and the first such thing is noted
+ * in err, which asl_pages_status reads.  Every array of slots' values has max_seqs entries, one per slot. */
+typedef struct {
+  int32_t n_layers;       /* layers whose rows the pages hold                                    */
+  int32_t n_kv_heads;     /* H_k                                                                 */
+  int32_t head_dim;       /* d (128 in this build)                                               */
+  int32_t page_size;      /* tokens of a page: 16, 32, 64 or 128                                 */
+  int32_t n_pages;        /* pages of the pool, at most 2^20, and n_pages * H_k * page_size < 2^31 */
+  int32_t max_seqs;       /* slots, at most 65536                                                */
+  int32_t max_pages;      /* length of a slot's row of the table; max_pages * page_size < 2^31   */
+  int32_t k_dtype;        /* ASL_K_BF16, or ASL_K_FP8_E4M3: K holds codes, the key is code x k_scale[layer][kv head] */
+  void* k;                /* device [n_layers][n_pages][H_k][page_size][d], bf16 or E4M3 codes, 16-byte aligned */
+  void* v;                /* device, the same in bf16                                            */
+  const float* k_scale;   /* device [n_layers][H_k]; read only for ASL_K_FP8_E4M3                */
+  int32_t* table;         /* device [max_seqs][max_pages]                                        */
+  int32_t* len;           /* device [max_seqs]                                                   */
+  int32_t* refs;          /* device [n_pages]                                                    */
+  int32_t* err;           /* device [2]: the first status noted and the slot (or pages missing)  */
+  int32_t* scratch;       /* device, asl_pages_scratch bytes, 16-byte aligned                    */
+  size_t scratch_bytes;
+} asl_pages;
+
+/* Sequences of one step.  Entry i is slot slots[i] and owns the packed tokens cu_q[i] .. cu_q[i+1]-1 of q, k, v and out:
+ * the last ones of the sequence, so that its token t (of n) stands at position len - n + t.  slots[i] = -1 (or any
+ * number that is no slot) is padding: its tokens, and those from cu_q[n_seqs] on, are left as they are. */
+typedef struct {
+  int32_t n_seqs;         /* at most 4096                                                        */
+  int32_t n_tokens;       /* rows that the buffers have room for; cu_q[n_seqs] <= n_tokens       */
+  const int32_t* slots;   /* device [n_seqs], each slot once                                     */
+  const int32_t* cu_q;    /* device [n_seqs + 1], cu_q[0] = 0, ascending                         */
+} asl_batch;
+
+/* Checks the description and reports the bytes of `scratch`.  ASL_ERR_INVALID, or ASL_ERR_UNSUPPORTED for a head_dim
+ * other than 128 and pools beyond the limits above. */
+asl_status asl_pages_scratch(const asl_pages* pages, size_t* bytes);
+
+/* Slot s grows to want[s] tokens (device int32 [max_seqs]; want[s] <= len[s], negative ones too: left as it is).  New pages
+ * are the lowest-numbered free ones, dealt out in the order of slots and of positions.  Where the slot's last page is
+ * not full and another slot holds it too, the slot gets a copy of the tokens that it has there, in all layers.  The
+ * new tokens' rows are whatever the pages held: asl_pages_append or asl_pages_store write them.  All or nothing: with
+ * too few free pages (ASL_ERR_PAGES, with the number missing) or a want beyond max_pages * page_size (ASL_ERR_INVALID,
+ * with the slot) no slot grows. */
+asl_status asl_pages_reserve(asl_ctx* ctx, const asl_pages* pages, const int32_t* want, void* stream);
+
+/* Slot s becomes a second holder of parent[s]'s pages (device int32 [max_seqs]; negative: left as it is).  No row is
+ * copied.  s has to be free, parent[s] another slot that is not itself forked in this call; else s is left as it is. */
+asl_status asl_pages_fork(asl_ctx* ctx, const asl_pages* pages, const int32_t* parent, void* stream);
+
+/* Slot s is cut to to[s] tokens, 0 frees it (device int32 [max_seqs]; negative or >= len[s]: left as it is).  Pages
+ * that no slot holds any more are free. */
+asl_status asl_pages_trim(asl_ctx* ctx, const asl_pages* pages, const int32_t* to, void* stream);
+
+/* Algorithm 1 (K[I], V[I]) into pages instead of dense buffers: token r of slot slots[b] gets row idx[h][kept_off_b + r]
+ * of request b, kv head by kv head (slots: device int32 [batch]; the plan, k, v and idx as in asl_compact_kv; the
+ * plan's H_k and k_dtype have to be the cache's).  The slots' pages come from an asl_pages_reserve before it; rows
+ * beyond a slot's length or into a page that another slot holds too are left out and noted. */
+asl_status asl_pages_store(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const void* k, const void* v,
+                           const int32_t* idx, const int32_t* slots, void* stream);
+
+/* Prunes cached sequences: token r of slot dst[j] gets row idx[h][off[j] + r] of slot src[j], r < off[j+1] - off[j],
+ * kv head by kv head (src, dst: device [n_jobs]; off: device [n_jobs + 1]; idx: device int32 [H_k][sum_kept], token
+ * positions as asl_select_topk writes them; max_kept: at least the longest list).  dst[j] is another slot than src[j],
+ * reserved before; asl_pages_trim then gives src[j] back.  Left out and noted: rows as in asl_pages_store, positions
+ * that src[j] does not have.  Each dst once. */
+asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const int32_t* src, const int32_t* dst,
+                             const int32_t* off, int32_t n_jobs, const int32_t* idx, int64_t sum_kept, int32_t max_kept,
+                             void* stream);
+
+/* Writes a step's K and V rows (device, packed [n_tokens][H_k][d]; element strides token, head; K as codes for
+ * ASL_K_FP8_E4M3) at their sequences' ends, which an asl_pages_reserve has made room for.  Left out and noted: tokens
+ * before a sequence's beginning, pages that another slot holds too. */
+asl_status asl_pages_append(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const asl_batch* batch, const void* k_new,
+                            const void* v_new, const int64_t k_stride[2], const int64_t v_stride[2], void* stream);
+
+/* Reads err (host-synchronising: waits for `stream` first).  ASL_OK, or the first status noted with *info set to its
+ * slot (ASL_ERR_PAGES: to the pages missing); err is cleared. */
+asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, int32_t* info);
+
+/* Attention of a step's tokens over their sequences' pages.  For query head a of token t at position p, with kv head
+ * h = a / (H_q / H_k) and x_j = q . k_j / sqrt(d):
+ *   lse = log sum_{j <= p} exp(x_j),   out = sum_{j <= p} exp(x_j - lse) v_j
+ * (what asl_score_layer_lse takes).  Rows behind a sequence's end, in its pages or not, count for nothing whatever
+ * they hold, and so do positions after p.  A token that sees no key (a free slot) has out = 0 and lse = -inf.
+ *
+ * asl_attend_plan reads table, len and the batch on the device and deals the work out; every asl_attend of the step,
+ * on any layer, uses it.  Plan again when a slot's length or pages, or the batch, have changed.  With `share` the plan
+ * looks for neighbours of the batch whose pages begin alike (forks of one prompt, side by side) and such a prefix is
+ * read once for all of them, their rows multiplied together; without it, or where little is shared, every sequence
+ * reads its own.  The workspace (asl_attend_workspace bytes, 256-byte aligned) carries the plan and the parts of rows
+ * whose keys are split over several blocks; calls that share it have to be ordered one behind another.
+ * H_q is a multiple of H_k with H_q / H_k <= 128. */
+asl_status asl_attend_workspace(const asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, size_t* bytes);
+asl_status asl_attend_plan(asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, int32_t share,
+                           void* workspace, size_t workspace_bytes, void* stream);
+/* q: device bf16 [n_tokens][H_q][d] (element strides token, head: multiples of 8); out: device bf16 dense
+ * [n_tokens][H_q][d]; lse: device fp32 [n_tokens][H_q], or null. */
+asl_status asl_attend(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const asl_batch* batch, int32_t n_q_heads,
+                      const void* q, const int64_t q_stride[2], void* out, float* lse, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
+/* asl_run_layer with its last step into pages: asl_pages_store on `side2` in asl_compact_kv's place (k_out and v_out of
+ * `layer` are not looked at).  `slots` as in asl_pages_store, reserved before on a stream that `stream` is ordered behind. */
+asl_status asl_run_layer_pages(asl_ctx* ctx, const asl_layer* layer, const asl_pages* pages, int32_t page_layer,
+                               const int32_t* slots, const void* q_obs, const void* k, const void* v, const float* lse,
+                               int32_t layer_idx, int32_t n_rows, int32_t slot);
 
 /* Number of kernels this context has launched so far (host counter). */
 int64_t asl_launch_count(const asl_ctx* ctx);

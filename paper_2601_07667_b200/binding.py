@@ -16,13 +16,16 @@ LIB_PATH = os.path.join(_HERE, "libasl_b200.so")
 ASL_POOL_AVG, ASL_POOL_MAX = 0, 1
 ASL_K_BF16, ASL_K_FP8_E4M3 = 0, 1
 ASL_OK, ASL_ERR_INVALID, ASL_ERR_UNSUPPORTED, ASL_ERR_WORKSPACE = 0, -1, -2, -3
-ASL_ERR_CUDA, ASL_ERR_TIMEOUT, ASL_ERR_ARCH = -4, -5, -6
+ASL_ERR_CUDA, ASL_ERR_TIMEOUT, ASL_ERR_ARCH, ASL_ERR_PAGES = -4, -5, -6, -7
 
 EXPORTS = ("asl_create", "asl_destroy", "asl_plan", "asl_plan_sizes", "asl_score_layer", "asl_rank_stat",
            "asl_select_topk", "asl_compact_kv", "asl_device_status", "asl_launch_count", "asl_strerror",
            "asl_rank_desc_static", "asl_score_layer_lse", "asl_window_lse", "asl_compact_rows",
            "asl_score_columns", "asl_pool_scores", "asl_set_controller", "asl_select_topk_gated",
-           "asl_selftest_bounded_wait", "asl_set_layer", "asl_run_layer", "asl_run_join", "asl_run_reset")
+           "asl_selftest_bounded_wait", "asl_set_layer", "asl_run_layer", "asl_run_join", "asl_run_reset",
+           "asl_pages_scratch", "asl_pages_reserve", "asl_pages_fork", "asl_pages_trim", "asl_pages_store",
+           "asl_pages_compact", "asl_pages_append", "asl_pages_status", "asl_attend_workspace", "asl_attend_plan",
+           "asl_attend", "asl_run_layer_pages")
 ASL_RANK_STATIC_MAX_T = 262144
 
 
@@ -41,6 +44,17 @@ class AslLayer(C.Structure):
                 ("scores_agg", C.c_void_p * 2), ("rank_ring", C.c_void_p), ("stat", C.c_void_p), ("idx", C.c_void_p),
                 ("k_out", C.c_void_p), ("v_out", C.c_void_p), ("stream", C.c_void_p), ("side", C.c_void_p),
                 ("side2", C.c_void_p), ("one_side", C.c_int32), ("reserved0", C.c_int32)]
+
+
+class AslPages(C.Structure):
+    _fields_ = [("n_layers", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("n_pages", C.c_int32), ("max_seqs", C.c_int32), ("max_pages", C.c_int32), ("k_dtype", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("table", C.c_void_p), ("len", C.c_void_p),
+                ("refs", C.c_void_p), ("err", C.c_void_p), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
+
+
+class AslBatch(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("slots", C.c_void_p), ("cu_q", C.c_void_p)]
 
 
 class AslStat(C.Structure):
@@ -90,6 +104,19 @@ def _load() -> C.CDLL:
     lib.asl_run_layer.argtypes = [vp, C.POINTER(AslLayer), vp, vp, vp, vp, i32, i32, i32]
     lib.asl_run_join.argtypes = [vp, vp]
     lib.asl_run_reset.argtypes = [vp]
+    pages, batch, two = C.POINTER(AslPages), C.POINTER(AslBatch), C.POINTER(i64)
+    lib.asl_pages_scratch.argtypes = [pages, C.POINTER(sz)]
+    lib.asl_pages_reserve.argtypes = [vp, pages, vp, vp]
+    lib.asl_pages_fork.argtypes = [vp, pages, vp, vp]
+    lib.asl_pages_trim.argtypes = [vp, pages, vp, vp]
+    lib.asl_pages_store.argtypes = [vp, pages, i32, vp, vp, vp, vp, vp]
+    lib.asl_pages_compact.argtypes = [vp, pages, i32, vp, vp, vp, i32, vp, i64, i32, vp]
+    lib.asl_pages_append.argtypes = [vp, pages, i32, batch, vp, vp, two, two, vp]
+    lib.asl_pages_status.argtypes = [vp, pages, vp, C.POINTER(i32)]
+    lib.asl_attend_workspace.argtypes = [vp, pages, batch, i32, C.POINTER(sz)]
+    lib.asl_attend_plan.argtypes = [vp, pages, batch, i32, i32, vp, sz, vp]
+    lib.asl_attend.argtypes = [vp, pages, i32, batch, i32, vp, two, vp, vp, vp, sz, vp]
+    lib.asl_run_layer_pages.argtypes = [vp, C.POINTER(AslLayer), pages, i32, vp, vp, vp, vp, vp, i32, i32, i32]
     lib.asl_launch_count.argtypes = [vp]
     lib.asl_launch_count.restype = i64
     lib.asl_strerror.argtypes = [C.c_int]
@@ -271,6 +298,64 @@ def asl_rank_desc_static(scores, T: int, rank_out, stream=None) -> None:
            "asl_rank_desc_static")
 
 
+def asl_pages_scratch(pages: AslPages) -> int:
+    size = C.c_size_t(0)
+    _check(_lib.asl_pages_scratch(C.byref(pages), C.byref(size)), "asl_pages_scratch")
+    return size.value
+
+
+def asl_pages_reserve(ctx, pages: AslPages, want, stream=None) -> None:
+    _check(_lib.asl_pages_reserve(ctx, pages, _ptr(want), _stream_handle(stream)), "asl_pages_reserve")
+
+
+def asl_pages_fork(ctx, pages: AslPages, parent, stream=None) -> None:
+    _check(_lib.asl_pages_fork(ctx, pages, _ptr(parent), _stream_handle(stream)), "asl_pages_fork")
+
+
+def asl_pages_trim(ctx, pages: AslPages, to, stream=None) -> None:
+    _check(_lib.asl_pages_trim(ctx, pages, _ptr(to), _stream_handle(stream)), "asl_pages_trim")
+
+
+def asl_pages_store(ctx, pages: AslPages, layer: int, k, v, idx, slots, stream=None) -> None:
+    _check(_lib.asl_pages_store(ctx, pages, int(layer), _ptr(k), _ptr(v), _ptr(idx), _ptr(slots), _stream_handle(stream)),
+           "asl_pages_store")
+
+
+def asl_pages_compact(ctx, pages: AslPages, layer: int, src, dst, off, n_jobs: int, idx, sum_kept: int, max_kept: int,
+                      stream=None) -> None:
+    _check(_lib.asl_pages_compact(ctx, pages, int(layer), _ptr(src), _ptr(dst), _ptr(off), int(n_jobs), _ptr(idx), int(sum_kept),
+                                  int(max_kept), _stream_handle(stream)), "asl_pages_compact")
+
+
+def asl_pages_append(ctx, pages: AslPages, layer: int, batch: AslBatch, k_new, v_new, k_stride, v_stride, stream=None) -> None:
+    _check(_lib.asl_pages_append(ctx, pages, int(layer), batch, _ptr(k_new), _ptr(v_new), (C.c_int64 * 2)(*k_stride),
+                                 (C.c_int64 * 2)(*v_stride), _stream_handle(stream)), "asl_pages_append")
+
+
+def asl_pages_status(ctx, pages: AslPages, stream=None):
+    info = C.c_int32(0)
+    st = _lib.asl_pages_status(ctx, pages, _stream_handle(stream), C.byref(info))
+    return st, info.value
+
+
+def asl_attend_workspace(ctx, pages: AslPages, batch: AslBatch, n_q_heads: int) -> int:
+    size = C.c_size_t(0)
+    _check(_lib.asl_attend_workspace(ctx, pages, batch, int(n_q_heads), C.byref(size)), "asl_attend_workspace")
+    return size.value
+
+
+def asl_attend_plan(ctx, pages: AslPages, batch: AslBatch, n_q_heads: int, share: bool, workspace, workspace_bytes: int,
+                    stream=None) -> None:
+    _check(_lib.asl_attend_plan(ctx, pages, batch, int(n_q_heads), int(share), _ptr(workspace), int(workspace_bytes),
+                                _stream_handle(stream)), "asl_attend_plan")
+
+
+def asl_attend(ctx, pages: AslPages, layer: int, batch: AslBatch, n_q_heads: int, q, q_stride, out, lse, workspace,
+               workspace_bytes: int, stream=None) -> None:
+    _check(_lib.asl_attend(ctx, pages, int(layer), batch, int(n_q_heads), _ptr(q), (C.c_int64 * 2)(*q_stride), _ptr(out), _ptr(lse),
+                           _ptr(workspace), int(workspace_bytes), _stream_handle(stream)), "asl_attend")
+
+
 # ---- a small holder of one plan's device buffers -------------------------------------
 class LayerPath:
     """Owns a context, its plan and the device buffers of one layer's pass
@@ -328,6 +413,13 @@ class LayerPath:
         self._layer_ref = C.byref(self._layer)
         self.first_layer: Optional[int] = None
         self.latch = False
+        self._pages = None                              # (PagedCache, slots): see store_into
+
+    def store_into(self, cache: Optional["PagedCache"], slots=None) -> None:
+        """From now on ``run_layer`` stores the kept rows into ``cache`` (layer ``layer_idx`` of it) instead of ``k_out`` and
+        ``v_out``: request b's into slot ``slots[b]`` (device int32 [batch]), which ``cache.reserve`` has grown to ``kept[b]``
+        tokens on the stream of the layers.  ``None``: into ``k_out`` and ``v_out`` again."""
+        self._pages = None if cache is None else (cache, slots)
 
     def set_controller(self, mode: int) -> None:
         """ASL_CONTROLLER_LATCH: selections are final on the device and ``run_layer`` tells the library the
@@ -409,8 +501,13 @@ class LayerPath:
             e0.record()
         if overlap:
             self._layer.stream = main
-            status = _lib.asl_run_layer(self.ctx, self._layer_ref, q_obs.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                        _ptr(lse), layer_idx, rows, self._cur)
+            if self._pages is None:
+                status = _lib.asl_run_layer(self.ctx, self._layer_ref, q_obs.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                            _ptr(lse), layer_idx, rows, self._cur)
+            else:
+                cache, slots = self._pages
+                status = _lib.asl_run_layer_pages(self.ctx, self._layer_ref, cache.pages, layer_idx, _ptr(slots), q_obs.data_ptr(),
+                                                  k.data_ptr(), v.data_ptr(), _ptr(lse), layer_idx, rows, self._cur)
             if status != ASL_OK:
                 raise AslError(status, "asl_run_layer")
         else:
@@ -425,9 +522,168 @@ class LayerPath:
         asl_pool_scores(ctx, ws, wsb, self._cur, skv, agg, main)
         asl_rank_stat(ctx, agg, layer_idx, rows, self.rank_ring, self.stat, ws, wsb, main)
         asl_select_topk(ctx, skv, self.H_k, self.idx, ws, wsb, main)
-        asl_compact_kv(ctx, k, v, self.idx, self.k_out, self.v_out, main)
+        if self._pages is None:
+            asl_compact_kv(ctx, k, v, self.idx, self.k_out, self.v_out, main)
+        else:
+            asl_pages_store(ctx, self._pages[0].pages, layer_idx, k, v, self.idx, self._pages[1], main)
 
     def read_stat(self) -> np.ndarray:
         """Device -> host copy of the [B] statistic records (synchronises)."""
         self.join()
         return self.stat.cpu().numpy().view(STAT_DTYPE).reshape(self.batch)
+
+
+class Batch:
+    """The sequences of one step (see ``PagedCache.batch``): the descriptor, and the workspace of its attention."""
+
+    def __init__(self, cache: "PagedCache", slots, cu_q, n_tokens: int, n_q_heads: Optional[int]):
+        self.slots, self.cu_q = cache._ints(slots, "slots"), cache._ints(cu_q, "cu_q")
+        if len(self.cu_q) != len(self.slots) + 1:
+            raise AslError(ASL_ERR_INVALID, "batch: cu_q has one entry more than slots")
+        self.n_tokens, self.n_q_heads = int(n_tokens), n_q_heads
+        self.desc = AslBatch(len(self.slots), self.n_tokens, _ptr(self.slots), _ptr(self.cu_q))
+        self.workspace, self.ws_bytes = None, 0
+        if n_q_heads is not None:
+            self.ws_bytes = asl_attend_workspace(cache.ctx, cache.pages, self.desc, n_q_heads)
+            self.workspace = cache.torch.empty(self.ws_bytes, dtype=cache.torch.uint8, device=cache.dev)
+
+
+class PagedCache:
+    """Pages of K and V for several layers, the slots' table, lengths and counts, all torch tensors, and the calls on them
+    (``asl_pages_*``, ``asl_attend*``) on the current stream.  Made from sizes, or over tensors that the caller already
+    has (``k``, ``v`` [n_layers][n_pages][H_k][page_size][d], ``table`` [max_seqs][max_pages], ``length`` [max_seqs],
+    ``refs`` [n_pages]; ``k`` of one-byte elements are E4M3 codes with ``k_scale`` [n_layers][H_k]).
+
+    ``reserve(want)``, ``fork(parent)`` and ``trim(to)`` take one int32 per slot on the device (negative: leave the slot
+    alone).  What does not fit is left out on the device and noted; ``check()`` waits and raises it."""
+
+    def __init__(self, *, page_size: int, n_layers: int = 1, n_kv_heads: int = 0, head_dim: int = 128, n_pages: int = 0,
+                 max_seqs: int = 0, max_pages: int = 0, k_dtype: int = ASL_K_BF16, k_scale=None, device: int = 0,
+                 k=None, v=None, table=None, length=None, refs=None):
+        import torch
+        self.torch = torch
+        if k is None:
+            dev = torch.device("cuda", device)
+            shape = (n_layers, n_pages, n_kv_heads, page_size, head_dim)
+            if min(shape) < 1 or max_seqs < 1 or max_pages < 1:
+                raise AslError(ASL_ERR_INVALID, "PagedCache: sizes")
+            k = torch.zeros(shape, dtype=torch.uint8 if k_dtype == ASL_K_FP8_E4M3 else torch.bfloat16, device=dev)
+            v = torch.zeros(shape, dtype=torch.bfloat16, device=dev)
+            table = torch.zeros((max_seqs, max_pages), dtype=torch.int32, device=dev)
+            length = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
+            refs = torch.zeros(n_pages, dtype=torch.int32, device=dev)
+        self.dev, self.ctx = k.device, 0
+        if k.dim() != 5 or v.shape != k.shape or k.shape[3] != page_size or v.dtype != torch.bfloat16 or table.dim() != 2:
+            raise AslError(ASL_ERR_INVALID, "PagedCache: k and v are [n_layers][n_pages][H_k][page_size][d]")
+        if k.element_size() == 1:
+            k_dtype = ASL_K_FP8_E4M3
+        elif k.dtype != torch.bfloat16:
+            raise AslError(ASL_ERR_INVALID, "PagedCache: k is bf16 or one-byte codes")
+        else:
+            k_dtype = ASL_K_BF16
+        if not (k.is_contiguous() and v.is_contiguous() and v.device == k.device):
+            raise AslError(ASL_ERR_INVALID, "PagedCache: k and v are dense, on one device")
+        self.k, self.v = k, v
+        self.table, self.len, self.refs = self._ints(table, "table"), self._ints(length, "length"), self._ints(refs, "refs")
+        if self.len.numel() != table.shape[0] or self.refs.numel() != k.shape[1]:
+            raise AslError(ASL_ERR_INVALID, "PagedCache: one length per slot, one count per page")
+        self.k_scale = None
+        if k_dtype == ASL_K_FP8_E4M3:
+            self.k_scale = torch.as_tensor(k_scale if k_scale is not None else [], dtype=torch.float32, device=self.dev).contiguous()
+            if tuple(self.k_scale.shape) != (k.shape[0], k.shape[2]):
+                raise AslError(ASL_ERR_INVALID, "PagedCache: k_scale is [n_layers][H_k]")
+        self.err = torch.zeros(2, dtype=torch.int32, device=self.dev)
+        self.pages = AslPages(k.shape[0], k.shape[2], k.shape[4], page_size, k.shape[1], table.shape[0], table.shape[1], k_dtype,
+                              _ptr(k), _ptr(v), _ptr(self.k_scale), _ptr(self.table), _ptr(self.len), _ptr(self.refs),
+                              _ptr(self.err), None, 0)
+        self.pages.scratch_bytes = asl_pages_scratch(self.pages)
+        self.scratch = torch.empty(self.pages.scratch_bytes, dtype=torch.uint8, device=self.dev)
+        self.pages.scratch = _ptr(self.scratch)
+        self.ctx = asl_create(self.dev.index or 0)
+
+    def _ints(self, x, what: str):
+        if x.dtype != self.torch.int32 or not x.is_contiguous() or x.device != self.dev:
+            raise AslError(ASL_ERR_INVALID, f"{what}: dense int32 on the cache's device")
+        return x
+
+    def _per_slot(self, x, what: str):
+        if x.numel() != self.pages.max_seqs:
+            raise AslError(ASL_ERR_INVALID, f"{what}: one value per slot")
+        return self._ints(x, what)
+
+    def _rows(self, x, what: str, n_tokens: int, heads: int, bytes_: int = 2):
+        """A [tokens][heads][d] tensor's strides."""
+        if x.dim() != 3 or x.shape[0] < n_tokens or x.shape[1] != heads or x.shape[2] != self.pages.head_dim or x.stride(2) != 1:
+            raise AslError(ASL_ERR_INVALID, f"{what}: [tokens][heads][d] with dense rows")
+        if x.element_size() != bytes_ or x.device != self.dev:
+            raise AslError(ASL_ERR_INVALID, f"{what}: element type or device")
+        return x.stride(0), x.stride(1)
+
+    def batch(self, slots, cu_q, n_tokens: int, n_q_heads: Optional[int] = None) -> Batch:
+        """Sequences of a step: entry i is slot ``slots[i]`` (-1: padding) and owns tokens ``cu_q[i]`` .. ``cu_q[i+1]``, its last ones
+        (device int32, read at every call).  ``n_q_heads``: also make the workspace that ``plan`` and ``attend`` need."""
+        return Batch(self, slots, cu_q, n_tokens, n_q_heads)
+
+    def reserve(self, want) -> None:
+        asl_pages_reserve(self.ctx, self.pages, self._per_slot(want, "want"))
+
+    def fork(self, parent) -> None:
+        asl_pages_fork(self.ctx, self.pages, self._per_slot(parent, "parent"))
+
+    def trim(self, to) -> None:
+        asl_pages_trim(self.ctx, self.pages, self._per_slot(to, "to"))
+
+    def store(self, layer: int, path: LayerPath, k, v, idx, slots) -> None:
+        """The kept rows of ``path``'s requests (``idx`` as its top-k wrote them) into layer ``layer`` of the slots."""
+        asl_pages_store(path.ctx, self.pages, layer, k, v, self._ints(idx, "idx"), self._ints(slots, "slots"))
+
+    def compact(self, layer: int, src, dst, off, idx, max_kept: int) -> None:
+        """Token r of slot ``dst[j]`` gets row ``idx[h][off[j] + r]`` of slot ``src[j]``; ``idx`` [H_k][kept of all jobs]."""
+        if idx.dim() != 2 or idx.shape[0] != self.pages.n_kv_heads or len(off) != len(src) + 1 or len(dst) != len(src):
+            raise AslError(ASL_ERR_INVALID, "compact: idx is [H_k][sum_kept], off has one entry more than src and dst")
+        asl_pages_compact(self.ctx, self.pages, layer, self._ints(src, "src"), self._ints(dst, "dst"), self._ints(off, "off"),
+                          len(src), self._ints(idx, "idx"), idx.shape[1], max_kept)
+
+    def append(self, layer: int, batch: Batch, k_new, v_new) -> None:
+        """K and V rows [n_tokens][H_k][d] of the batch's tokens, to the ends of their sequences."""
+        H = self.pages.n_kv_heads
+        ks = self._rows(k_new, "k_new", batch.n_tokens, H, self.k.element_size())
+        vs = self._rows(v_new, "v_new", batch.n_tokens, H)
+        asl_pages_append(self.ctx, self.pages, layer, batch.desc, k_new, v_new, ks, vs)
+
+    def plan(self, batch: Batch, share: bool = True) -> None:
+        """Deals out the attention of the step; again whenever lengths, pages or the batch have changed."""
+        asl_attend_plan(self.ctx, self.pages, batch.desc, batch.n_q_heads or 0, share, batch.workspace, batch.ws_bytes)
+
+    def attend(self, layer: int, batch: Batch, q, out=None, lse=None):
+        """Attention of the batch's tokens, q [n_tokens][H_q][d] bf16, over their sequences; out likewise (dense), lse
+        [n_tokens][H_q] fp32 or None.  Returns out."""
+        strides = self._rows(q, "q", batch.n_tokens, batch.n_q_heads or 0)
+        if out is None:
+            out = self.torch.empty((batch.n_tokens, batch.n_q_heads, self.pages.head_dim), dtype=q.dtype, device=self.dev)
+        elif not out.is_contiguous() or out.numel() < batch.n_tokens * batch.n_q_heads * self.pages.head_dim or out.element_size() != 2:
+            raise AslError(ASL_ERR_INVALID, "out: dense [n_tokens][H_q][d] bf16")
+        if lse is not None and (not lse.is_contiguous() or lse.numel() < batch.n_tokens * batch.n_q_heads or lse.element_size() != 4):
+            raise AslError(ASL_ERR_INVALID, "lse: dense [n_tokens][H_q] fp32")
+        asl_attend(self.ctx, self.pages, layer, batch.desc, batch.n_q_heads, q, strides, out, lse, batch.workspace, batch.ws_bytes)
+        return out
+
+    def check(self) -> None:
+        """Waits for the current stream and raises what the calls so far have noted."""
+        st, info = asl_pages_status(self.ctx, self.pages)
+        if st != ASL_OK:
+            raise AslError(st, f"paged cache ({'pages missing' if st == ASL_ERR_PAGES else 'slot'} {info})")
+        st, where = asl_device_status(self.ctx)
+        if st != ASL_OK:
+            raise AslError(st, f"device wait {where}")
+
+    def close(self) -> None:
+        if self.ctx:
+            asl_destroy(self.ctx)
+            self.ctx = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

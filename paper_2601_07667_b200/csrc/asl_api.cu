@@ -283,8 +283,9 @@ asl_status asl_set_layer(asl_ctx* c, int32_t layer_idx) {
   return ASL_OK;
 }
 
-// what follows the scoring of a layer, on its side streams
-static asl_status issue_tail(asl_ctx* c, const asl_layer* l, const void* k, const void* v, int32_t layer_idx, int32_t n_rows, int32_t slot) {
+// what follows the scoring of a layer, on its side streams; `last`: what stands in compaction's place, or null
+static asl_status issue_tail(asl_ctx* c, const asl_layer* l, const void* k, const void* v, int32_t layer_idx, int32_t n_rows, int32_t slot,
+                             asl_last_step last, const void* last_arg) {
   const cudaStream_t s1 = static_cast<cudaStream_t>(l->side), s2 = static_cast<cudaStream_t>(l->side2);
   asl_status st = asl_pool_scores(c, l->workspace, l->workspace_bytes, slot, l->scores_kv[slot], l->scores_agg[slot], l->side);
   if (st != ASL_OK) return st;
@@ -294,11 +295,13 @@ static asl_status issue_tail(asl_ctx* c, const asl_layer* l, const void* k, cons
   if (st != ASL_OK) return st;
   st = asl_select_topk(c, l->scores_kv[slot], c->p.n_kv_heads, l->idx, l->workspace, l->workspace_bytes, l->side2);
   if (st != ASL_OK) return st;
-  return asl_compact_kv(c, k, v, l->idx, l->k_out, l->v_out, l->side2);
+  return last ? last(c, l, k, v, last_arg) : asl_compact_kv(c, k, v, l->idx, l->k_out, l->v_out, l->side2);
 }
 
-asl_status asl_run_layer(asl_ctx* c, const asl_layer* l, const void* q_obs, const void* k, const void* v, const float* lse,
-                         int32_t layer_idx, int32_t n_rows, int32_t slot) {
+}  // extern "C"
+
+asl_status asl_run_layer_last(asl_ctx* c, const asl_layer* l, const void* q_obs, const void* k, const void* v, const float* lse,
+                              int32_t layer_idx, int32_t n_rows, int32_t slot, asl_last_step last, const void* last_arg) {
   if (!c || !l || slot < 0 || slot > 1) return ASL_ERR_INVALID;
   const cudaStream_t main = static_cast<cudaStream_t>(l->stream), s1 = static_cast<cudaStream_t>(l->side), s2 = static_cast<cudaStream_t>(l->side2);
   if (c->pending[slot])                             // the work of two layers ago has read the slot's buffers
@@ -307,7 +310,7 @@ asl_status asl_run_layer(asl_ctx* c, const asl_layer* l, const void* q_obs, cons
   if (st != ASL_OK) return st;
   ASL_CUDA(cudaEventRecord(c->ev_scored, main));
   ASL_CUDA(cudaStreamWaitEvent(s1, c->ev_scored, 0));
-  st = issue_tail(c, l, k, v, layer_idx, n_rows, slot);
+  st = issue_tail(c, l, k, v, layer_idx, n_rows, slot, last, last_arg);
   // a step that fails leaves those before it queued: the slot's next use and a join wait for them as for a whole layer
   if (st != ASL_OK) ASL_CUDA(cudaStreamWaitEvent(s2, c->ev_scored, 0));        // (a capture may not have reached s2 yet)
   ASL_CUDA(cudaEventRecord(c->ev_done[slot][1], s2));
@@ -316,6 +319,13 @@ asl_status asl_run_layer(asl_ctx* c, const asl_layer* l, const void* q_obs, cons
   c->pending[slot] = true;
   c->last_slot = slot;
   return st;
+}
+
+extern "C" {
+
+asl_status asl_run_layer(asl_ctx* c, const asl_layer* l, const void* q_obs, const void* k, const void* v, const float* lse,
+                         int32_t layer_idx, int32_t n_rows, int32_t slot) {
+  return asl_run_layer_last(c, l, q_obs, k, v, lse, layer_idx, n_rows, slot, nullptr, nullptr);
 }
 
 asl_status asl_run_join(asl_ctx* c, void* stream) {
@@ -375,6 +385,7 @@ const char* asl_strerror(asl_status s) {
     case ASL_ERR_CUDA: return "CUDA call failed";
     case ASL_ERR_TIMEOUT: return "bounded device wait expired";
     case ASL_ERR_ARCH: return "device is not sm_100";
+    case ASL_ERR_PAGES: return "too few free pages";
   }
   return "unknown status";
 }

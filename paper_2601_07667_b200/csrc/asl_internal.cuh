@@ -149,4 +149,9 @@ asl_status asl_launch_compact(asl_ctx* c, const void* k, const void* v, const in
 asl_status asl_launch_compact_rows(asl_ctx* c, const void* x, const int32_t* idx, void* out, int64_t row_bytes,
                                    cudaStream_t st);
 
+// asl_run_layer with another last step than asl_compact_kv, on the layer's side2 (null: that one)
+typedef asl_status (*asl_last_step)(asl_ctx* c, const asl_layer* l, const void* k, const void* v, const void* arg);
+asl_status asl_run_layer_last(asl_ctx* c, const asl_layer* l, const void* q_obs, const void* k, const void* v, const float* lse,
+                              int32_t layer_idx, int32_t n_rows, int32_t slot, asl_last_step last, const void* last_arg);
+
 constexpr int ASL_RANK_TILE = 2048;      // keys per block in the radix sort

@@ -1,0 +1,460 @@
+// Attention over pages: the plan, the rows whose parts are put together, and the entry points.
+#include <math.h>
+
+#include "asl_ptx.cuh"
+#include "attend.cuh"
+
+namespace {
+
+constexpr int PLAN_THREADS = 512;
+constexpr int NARROW_CTAS = 2;             // per SM
+// Least keys that a prefix saves (its length times all its readers but one) for it to be read by the group: below, one more
+// launch with work and one more part per row cost more than the copies of it in L2.
+constexpr int SHARE_MIN_KEYS = 1024;
+
+// Leading pages that an entry of the batch has in common with the one before it; only pages that both hold in full.
+__global__ void __launch_bounds__(128) attend_same_kernel(PagePool g, asl_batch b, int32_t* same) {
+  pdl_wait_predecessor();
+  const int i = blockIdx.x;
+  int m = 0;
+  if (i > 0) {
+    const int s = __ldcg(b.slots + i), r = __ldcg(b.slots + i - 1);
+    if ((unsigned)s < (unsigned)g.max_seqs && (unsigned)r < (unsigned)g.max_seqs)
+      m = min(min(__ldcg(g.len + s), __ldcg(g.len + r)) >> g.page_shift, g.max_pages);
+    const int32_t* x = g.table + (int64_t)s * g.max_pages;
+    const int32_t* y = g.table + (int64_t)r * g.max_pages;
+    for (int j0 = 0; j0 < m; j0 += 128) {
+      const int j = j0 + threadIdx.x;
+      const bool differs = j < m && __ldcg(x + j) != __ldcg(y + j);
+      const unsigned any = __ballot_sync(0xffffffffu, differs);
+      __shared__ int first[4];
+      if ((threadIdx.x & 31) == 0) first[threadIdx.x >> 5] = any ? j0 + threadIdx.x + __ffs(any) - 1 : m;
+      __syncthreads();
+      m = min(m, min(min(first[0], first[1]), min(first[2], first[3])));
+      __syncthreads();
+    }
+  }
+  if (threadIdx.x == 0) same[i] = max(m, 0);
+}
+
+__device__ __forceinline__ int scan_step(int v, int* part, int& total) {       // as block_scan, 512 threads
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int s = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += u;
+  }
+  if (lane == 31) part[warp] = s;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int k = 0; k < PLAN_THREADS / 32; ++k) {
+    if (k < warp) before += part[k];
+    total += part[k];
+  }
+  __syncthreads();
+  return before + s - v;
+}
+
+struct PlanArgs {
+  PagePool g;
+  asl_batch b;
+  AttendPtrs w;
+  int32_t G, n_q_heads, share, narrow_grid, wide_grid;
+};
+
+// One block: groups of neighbours, prefix sums over sequences and groups, and where every CTA's stretch begins.
+__global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
+  extern __shared__ int32_t sm[];          // per sequence: ntok, len, group, then first narrow tile (one more at the end)
+  __shared__ int part[PLAN_THREADS / 32];
+  __shared__ int n_groups_s, bad;
+  pdl_wait_predecessor();
+  const int tid = threadIdx.x, n = a.b.n_seqs, G = a.G;
+  int32_t* ntok = sm;
+  int32_t* len = sm + n;
+  int32_t* grp = sm + 2 * n;
+  int32_t* first = sm + 3 * n;             // [n + 1]
+  int32_t* gpfx = first + n + 1;           // per group: shared tokens, first entry, wide cost before
+  int32_t* gat = gpfx + n;
+  int32_t* gcost = gat + n;                // [n + 1]
+  if (tid == 0) a.w.head->made_for[0] = 0;
+  for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tok_seq[t] = -1;
+  for (int i = tid; i < n; i += PLAN_THREADS) {
+    const int s = __ldcg(a.b.slots + i), t0 = __ldcg(a.b.cu_q + i), t1 = __ldcg(a.b.cu_q + i + 1);
+    const bool slot_ok = (unsigned)s < (unsigned)a.g.max_seqs, tok_ok = t0 >= 0 && t1 >= t0 && t1 <= a.b.n_tokens;
+    if (slot_ok && !tok_ok) note_error(a.g.err, ASL_ERR_INVALID, s);
+    ntok[i] = slot_ok && tok_ok ? t1 - t0 : 0;
+    len[i] = ntok[i] ? min(max(__ldcg(a.g.len + s), 0), a.g.max_pages << a.g.page_shift) : 0;
+  }
+  __syncthreads();
+  // Groups: an entry joins the group before it where that group then saves no less than without it.
+  if (tid == 0) {
+    int ng = 0, held = 0, keys = 0;                          // of the open group: entries, and its shared tokens
+    int64_t most = 0;                                        // tiles, were nothing shared: they are counted in 32 bits
+    bool open = false;
+    for (int i = 0; i < n; ++i) {
+      if (ntok[i] == 0) { grp[i] = -1; open = false; continue; }
+      most += (int64_t)narrow_chunks_of(ntok[i], G) * (len[i] / NARROW_KEYS + 2);
+      const int own = max(0, len[i] - ntok[i]) >> a.g.page_shift << a.g.page_shift;     // all its tokens see these
+      const int both = open && a.share ? min(min(keys, own), __ldcg(a.w.same + i) << a.g.page_shift) : 0;
+      if (both > 0 && (int64_t)held * both >= (int64_t)(held - 1) * keys) {
+        keys = both;
+        ++held;
+      } else {
+        gat[ng++] = i;
+        held = 1;
+        keys = own;
+        open = true;
+      }
+      grp[i] = ng - 1;
+      gpfx[ng - 1] = held > 1 && (int64_t)(held - 1) * keys >= SHARE_MIN_KEYS ? keys : 0;
+    }
+    n_groups_s = ng;
+    bad = most >= 1 << 30;
+    if (bad) note_error(a.g.err, ASL_ERR_UNSUPPORTED, -1);
+  }
+  __syncthreads();
+  if (bad) return;
+  const int ng = n_groups_s;
+  int tiles = 0, chunks = 0;
+  for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
+    const int i = i0 + tid;
+    int nt = 0, nc = 0, pfx = 0;
+    if (i < n && ntok[i]) {
+      pfx = gpfx[grp[i]];
+      nc = narrow_chunks_of(ntok[i], G);
+      nt = nc * max(1, (len[i] - pfx + NARROW_KEYS - 1) / NARROW_KEYS);
+    }
+    int tsum, csum;
+    const int t0 = tiles + scan_step(nt, part, tsum), c0 = chunks + scan_step(nc, part, csum);
+    if (i < n) {
+      first[i] = t0;
+      AttendSeq s;
+      s.tok0 = __ldcg(a.b.cu_q + i);
+      s.ntok = ntok[i];
+      s.slot = ntok[i] ? __ldcg(a.b.slots + i) : -1;
+      s.len = len[i];
+      s.pfx = pfx;
+      s.tile0 = t0;
+      s.chunk0 = c0;
+      s.group = grp[i];
+      a.w.seqs[i] = s;
+      for (int t = 0; t < ntok[i]; ++t) a.w.tok_seq[s.tok0 + t] = i;
+    }
+    tiles += tsum;
+    chunks += csum;
+  }
+  int cost = 0, wchunks = 0;
+  for (int i0 = 0; i0 < ng; i0 += PLAN_THREADS) {
+    const int i = i0 + tid;
+    int c = 0, nc = 0, tokens = 0, at = 0, last = 0;
+    if (i < ng) {
+      at = gat[i];
+      last = i + 1 < ng ? gat[i + 1] : n;
+      while (last > at + 1 && ntok[last - 1] == 0) --last;      // padding behind the group
+      tokens = __ldcg(a.b.cu_q + last - 1) + ntok[last - 1] - __ldcg(a.b.cu_q + at);
+      if (gpfx[i]) {
+        c = wide_group_cost(tokens, gpfx[i], G);
+        nc = (tokens + wide_tokens(G) - 1) / wide_tokens(G);
+      }
+    }
+    int csum, nsum;
+    const int c0 = cost + scan_step(c, part, csum), n0 = wchunks + scan_step(nc, part, nsum);
+    if (i < ng) {
+      gcost[i] = c0;
+      AttendGroup r;
+      r.tok0 = __ldcg(a.b.cu_q + at);
+      r.ntok = tokens;
+      r.slot = __ldcg(a.b.slots + at);
+      r.pfx = gpfx[i];
+      r.cost0 = c0;
+      r.chunk0 = n0;
+      r.pad0 = r.pad1 = 0;
+      a.w.groups[i] = r;
+    }
+    cost += csum;
+    wchunks += nsum;
+  }
+  if (tid == 0) { first[n] = tiles; gcost[ng] = cost; }
+  __syncthreads();
+  const int H = a.g.n_kv_heads;
+  const int narrow_each = (int)(((int64_t)H * tiles + a.narrow_grid - 1) / a.narrow_grid);
+  const int wide_each = max(2, (int)(((int64_t)H * cost + a.wide_grid - 1) / a.wide_grid));
+  for (int k = tid; k < a.narrow_grid; k += PLAN_THREADS) {
+    AttendStart s = {-1, 0, 0, 0};
+    const int64_t u = (int64_t)k * narrow_each;
+    if (u < (int64_t)H * tiles) {
+      s.h = (int)(u / tiles);
+      const int r = (int)(u % tiles);
+      int lo = 0, hi = n;                                       // last entry with first <= r that has tiles
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (first[mid] <= r) lo = mid; else hi = mid;
+      }
+      s.item = lo;
+      const int nt = max(1, (len[lo] - gpfx[grp[lo]] + NARROW_KEYS - 1) / NARROW_KEYS);
+      s.chunk = (r - first[lo]) / nt;
+      s.tile = (r - first[lo]) % nt;
+    }
+    a.w.narrow_start[k] = s;
+  }
+  for (int k = tid; k < a.wide_grid; k += PLAN_THREADS) {
+    AttendStart s = {-1, 0, 0, 0};
+    const int64_t u = (int64_t)k * wide_each;
+    if (u < (int64_t)H * cost) {
+      s.h = (int)(u / cost);
+      const int r = (int)(u % cost);
+      int lo = 0, hi = ng;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (gcost[mid] <= r) lo = mid; else hi = mid;
+      }
+      s.item = lo;
+      const int nt = (gpfx[lo] + WIDE_KEYS - 1) / WIDE_KEYS, T = wide_tokens(G), w = T * G > WIDE_ROWS / 2 ? 2 : 1;
+      int x = r - gcost[lo];
+      // full chunks first; the last one may count less
+      const int last = lo + 1 < ng ? gat[lo + 1] : n;
+      int e = last;
+      while (e > gat[lo] + 1 && ntok[e - 1] == 0) --e;
+      const int tokens = __ldcg(a.b.cu_q + e - 1) + ntok[e - 1] - __ldcg(a.b.cu_q + gat[lo]), whole = tokens / T;
+      s.chunk = min(x / (nt * w), whole);
+      x -= s.chunk * nt * w;
+      const int wl = s.chunk < whole ? w : (tokens % T) * G > WIDE_ROWS / 2 ? 2 : 1;
+      s.tile = (x + wl - 1) / wl;                               // the first tile that begins in the stretch
+      if (s.tile >= nt) s.h = -2;                               // begins with the chunk after: see wide_begin
+    }
+    a.w.wide_start[k] = s;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    AttendHead* h = a.w.head;
+    h->n_seqs = n;
+    h->n_groups = ng;
+    h->narrow_tiles = tiles;
+    h->narrow_chunks = chunks;
+    h->narrow_each = max(1, narrow_each);
+    h->wide_cost = cost;
+    h->wide_chunks = wchunks;
+    h->wide_each = wide_each;
+    h->made_for[0] = ATTEND_MARK;
+    h->made_for[1] = n;
+    h->made_for[2] = a.b.n_tokens;
+    h->made_for[3] = a.n_q_heads;
+    h->made_for[4] = a.g.n_kv_heads;
+  }
+}
+
+// Rows whose keys were split: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m the largest m_i, and the same for lse.  A
+// warp a row, four channels a lane; parts in a fixed order, so that a row comes out the same on every run.
+__global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
+  pdl_wait_predecessor();
+  if (!plan_fits(a)) return;
+  const int lane = threadIdx.x & 31;
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= a.n_tokens * a.n_q_heads) return;
+  const int t = row / a.n_q_heads, head = row % a.n_q_heads, G = a.group_heads, h = head / G, g = head % G;
+  const int i = __ldcg(a.w.tok_seq + t);
+  if (i < 0) return;
+  const AttendSeq s = load_seq(a.w.seqs + i);
+  const AttendHead* hd = a.w.head;
+  const int nt = narrow_tiles_of(s), lr = (t - s.tok0) * G + g, chunk = lr / NARROW_ROWS;
+  const int64_t each = __ldcg(&hd->narrow_each);
+  const int64_t ta = (int64_t)h * __ldcg(&hd->narrow_tiles) + s.tile0 + (int64_t)chunk * nt;
+  const int c0 = (int)(ta / each), c1 = (int)((ta + nt - 1) / each);
+  if (s.pfx == 0 && c0 == c1) return;                             // written where it was computed
+  const int64_t slot = (int64_t)h * __ldcg(&hd->narrow_chunks) + s.chunk0 + chunk;
+  // parts: narrow ones c0 .. c1, then those of the prefix (two halves each where a chunk's rows fill one)
+  const float2* ml[2];
+  const float* o[2];
+  int count[2], step[2];
+  ml[0] = a.w.narrow_ml + (slot + c0) * NARROW_ROWS + lr % NARROW_ROWS;
+  o[0] = a.w.narrow_o + ((slot + c0) * NARROW_ROWS + lr % NARROW_ROWS) * 128;
+  count[0] = c1 - c0 + 1;
+  step[0] = NARROW_ROWS;
+  count[1] = 0;
+  ml[1] = nullptr; o[1] = nullptr; step[1] = 0;
+  if (s.pfx) {
+    const AttendGroup gr = load_group(a.w.groups + s.group);
+    const int T = wide_tokens(G), ch = (t - gr.tok0) / T, wr = (t - gr.tok0) % T * G + g;
+    const int wt = (gr.pfx + WIDE_KEYS - 1) / WIDE_KEYS, w = wide_weight(gr, ch, G), w0 = T * G > WIDE_ROWS / 2 ? 2 : 1;
+    const int64_t we = __ldcg(&hd->wide_each);
+    const int64_t a0 = (int64_t)h * __ldcg(&hd->wide_cost) + gr.cost0 + (int64_t)ch * wt * w0;
+    const int x0 = (int)(a0 / we), x1 = (int)((a0 + (int64_t)(wt - 1) * w) / we);
+    const int64_t ws = (int64_t)h * __ldcg(&hd->wide_chunks) + gr.chunk0 + ch + x0;
+    const int halves = w == 1 ? 2 : 1;
+    step[1] = WIDE_ROWS / halves;
+    count[1] = (x1 - x0 + 1) * halves;
+    ml[1] = a.w.wide_ml + ws * WIDE_ROWS + wr;
+    o[1] = a.w.wide_o + (ws * WIDE_ROWS + wr) * 128;
+  }
+  const int total = count[0] + count[1];
+  auto entry = [&](int k) { return k < count[0] ? __ldcg(ml[0] + (int64_t)k * step[0]) : __ldcg(ml[1] + (int64_t)(k - count[0]) * step[1]); };
+  float top = -INFINITY;
+  for (int k = lane; k < total; k += 32) top = fmaxf(top, entry(k).x);
+#pragma unroll
+  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+  const float ref = top == -INFINITY ? 0.0f : top;
+  float sum = 0.0f;
+  float4 acc = make_float4(0, 0, 0, 0);
+  for (int k0 = 0; k0 < total; k0 += 32) {
+    const float2 e = k0 + lane < total ? entry(k0 + lane) : make_float2(-INFINITY, 0.0f);
+    const float f = ex2(e.x - ref);
+    sum += e.y * f;
+    const int m = min(32, total - k0);
+#pragma unroll 4
+    for (int k = 0; k < m; ++k) {
+      const float fk = __shfl_sync(0xffffffffu, f, k);
+      const float mk = __shfl_sync(0xffffffffu, e.x, k);
+      const int kk = k0 + k;
+      if (mk == -INFINITY) continue;                              // the part saw nothing: its result may be anything
+      const float* p = kk < count[0] ? o[0] + (int64_t)kk * step[0] * 128 : o[1] + (int64_t)(kk - count[0]) * step[1] * 128;
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + lane);
+      acc.x += v.x * fk; acc.y += v.y * fk; acc.z += v.z * fk; acc.w += v.w * fk;
+    }
+  }
+#pragma unroll
+  for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+  uint2 v;
+  v.x = *reinterpret_cast<uint32_t*>(&lo);
+  v.y = *reinterpret_cast<uint32_t*>(&hi);
+  *reinterpret_cast<uint2*>(a.out + (int64_t)row * 128 + lane * 4) = v;
+  if (a.lse && lane == 0) a.lse[row] = (ref + log2f(sum)) * 0.6931471805599453f;
+}
+
+AttendLayout layout_of(int sm_count, int n_kv_heads, int n_seqs, int n_tokens, int n_q_heads) {
+  AttendLayout l;
+  const int64_t G = n_q_heads / n_kv_heads, H = n_kv_heads;
+  l.narrow_grid = NARROW_CTAS * sm_count;
+  l.wide_grid = sm_count;
+  // chunks at most: of a sequence's rows one is not full; no more than every token's rows on their own
+  const int64_t per_token = (G + NARROW_ROWS - 1) / NARROW_ROWS;
+  int64_t narrow = n_tokens * G / NARROW_ROWS + n_seqs;
+  if (narrow > n_tokens * per_token) narrow = n_tokens * per_token;
+  const int64_t wide = n_tokens / wide_tokens((int)G) + n_seqs / 2 + 1;
+  const size_t narrow_slots = (size_t)(H * narrow + l.narrow_grid), wide_slots = (size_t)(H * wide + l.wide_grid);
+  size_t off = 0;
+  auto take = [&](size_t bytes) { const size_t at = off; off = asl_align256(off + bytes); return at; };
+  l.head = take(sizeof(AttendHead));
+  l.seqs = take(sizeof(AttendSeq) * n_seqs);
+  l.groups = take(sizeof(AttendGroup) * n_seqs);
+  l.same = take(sizeof(int32_t) * n_seqs);
+  l.tok_seq = take(sizeof(int32_t) * n_tokens);
+  l.narrow_start = take(sizeof(AttendStart) * l.narrow_grid);
+  l.wide_start = take(sizeof(AttendStart) * l.wide_grid);
+  l.narrow_ml = take(sizeof(float2) * NARROW_ROWS * narrow_slots);
+  l.narrow_o = take(sizeof(float) * 128 * NARROW_ROWS * narrow_slots);
+  l.wide_ml = take(sizeof(float2) * WIDE_ROWS * wide_slots);
+  l.wide_o = take(sizeof(float) * 128 * WIDE_ROWS * wide_slots);
+  l.total = off;
+  return l;
+}
+
+AttendPtrs ptrs_of(const AttendLayout& l, void* workspace) {
+  char* w = static_cast<char*>(workspace);
+  AttendPtrs p;
+  p.head = reinterpret_cast<AttendHead*>(w + l.head);
+  p.seqs = reinterpret_cast<AttendSeq*>(w + l.seqs);
+  p.groups = reinterpret_cast<AttendGroup*>(w + l.groups);
+  p.same = reinterpret_cast<int32_t*>(w + l.same);
+  p.tok_seq = reinterpret_cast<int32_t*>(w + l.tok_seq);
+  p.narrow_start = reinterpret_cast<AttendStart*>(w + l.narrow_start);
+  p.wide_start = reinterpret_cast<AttendStart*>(w + l.wide_start);
+  p.narrow_ml = reinterpret_cast<float2*>(w + l.narrow_ml);
+  p.narrow_o = reinterpret_cast<float*>(w + l.narrow_o);
+  p.wide_ml = reinterpret_cast<float2*>(w + l.wide_ml);
+  p.wide_o = reinterpret_cast<float*>(w + l.wide_o);
+  return p;
+}
+
+asl_status check_attend(const asl_ctx* c, const asl_pages* p, const asl_batch* b, int n_q_heads) {
+  if (!c) return ASL_ERR_INVALID;
+  const asl_status s = asl_check_pages(p);
+  if (s != ASL_OK) return s;
+  if (!b || !b->slots || !b->cu_q || b->n_seqs < 1 || b->n_tokens < 0) return ASL_ERR_INVALID;
+  if (n_q_heads < 1 || n_q_heads % p->n_kv_heads) return ASL_ERR_INVALID;
+  if (b->n_seqs > ATTEND_MAX_SEQS || n_q_heads / p->n_kv_heads > 128) return ASL_ERR_UNSUPPORTED;
+  if ((int64_t)b->n_tokens * n_q_heads >= (int64_t)1 << 31) return ASL_ERR_UNSUPPORTED;
+  return ASL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+asl_status asl_attend_workspace(const asl_ctx* c, const asl_pages* p, const asl_batch* b, int32_t n_q_heads, size_t* bytes) {
+  if (!bytes) return ASL_ERR_INVALID;
+  const asl_status s = check_attend(c, p, b, n_q_heads);
+  if (s == ASL_OK) *bytes = layout_of(c->sm_count, p->n_kv_heads, b->n_seqs, b->n_tokens, n_q_heads).total;
+  return s;
+}
+
+asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, int32_t n_q_heads, int32_t share, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  const asl_status s = check_attend(c, p, b, n_q_heads);
+  if (s != ASL_OK) return s;
+  if (!asl_on_device(c)) return ASL_ERR_INVALID;
+  const AttendLayout l = layout_of(c->sm_count, p->n_kv_heads, b->n_seqs, b->n_tokens, n_q_heads);
+  if (!workspace || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ASL_ERR_WORKSPACE;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  PlanArgs a;
+  a.g = page_pool(p, 0);
+  a.b = *b;
+  a.w = ptrs_of(l, workspace);
+  a.G = n_q_heads / p->n_kv_heads;
+  a.n_q_heads = n_q_heads;
+  a.share = 0 && share && b->n_seqs > 1;
+  a.narrow_grid = l.narrow_grid;
+  a.wide_grid = l.wide_grid;
+  const size_t smem = sizeof(int32_t) * (7 * (size_t)b->n_seqs + 2);
+  if (smem > 48 * 1024)
+    ASL_CUDA(cudaFuncSetAttribute(attend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (7 * ATTEND_MAX_SEQS + 2)));
+  if (a.share) {
+    launch_after(attend_same_kernel, dim3(b->n_seqs), dim3(128), st, a.g, a.b, a.w.same);
+    c->launches += 1;
+  }
+  launch_after_smem(attend_plan_kernel, dim3(1), dim3(PLAN_THREADS), smem, st, a);
+  c->launches += 1;
+  ASL_CUDA(cudaGetLastError());
+  return ASL_OK;
+}
+
+asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_batch* b, int32_t n_q_heads, const void* q,
+                      const int64_t q_stride[2], void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  asl_status s = check_attend(c, p, b, n_q_heads);
+  if (s != ASL_OK) return s;
+  if (!asl_on_device(c)) return ASL_ERR_INVALID;
+  if (layer < 0 || layer >= p->n_layers || !q || !out || !q_stride || !asl_aligned16(q) || !asl_aligned16(out)) return ASL_ERR_INVALID;
+  for (int i = 0; i < 2; ++i)
+    if (q_stride[i] < 0 || q_stride[i] % 8) return ASL_ERR_INVALID;
+  const AttendLayout l = layout_of(c->sm_count, p->n_kv_heads, b->n_seqs, b->n_tokens, n_q_heads);
+  if (!workspace || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ASL_ERR_WORKSPACE;
+  if (b->n_tokens == 0) return ASL_OK;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  AttendArgs a;
+  a.g = page_pool(p, layer);
+  a.w = ptrs_of(l, workspace);
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.qs_t = q_stride[0];
+  a.qs_h = q_stride[1];
+  a.out = static_cast<__nv_bfloat16*>(out);
+  a.lse = lse;
+  a.k_scale = p->k_dtype == ASL_K_FP8_E4M3 ? p->k_scale + (int64_t)layer * p->n_kv_heads : nullptr;
+  a.err = c->d_err;
+  a.n_q_heads = n_q_heads;
+  a.group_heads = n_q_heads / p->n_kv_heads;
+  a.n_tokens = b->n_tokens;
+  a.n_seqs = b->n_seqs;
+  a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p->head_dim));
+  s = asl_launch_attend_narrow(c, p, layer, a, l.narrow_grid, st);
+  if (s != ASL_OK) return s;
+  launch_after(attend_join_kernel, dim3((unsigned)(((int64_t)b->n_tokens * n_q_heads + 3) / 4)), dim3(128), st, a);
+  c->launches += 1;
+  ASL_CUDA(cudaGetLastError());
+  return ASL_OK;
+}
+
+}  // extern "C"

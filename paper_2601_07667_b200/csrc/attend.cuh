@@ -1,0 +1,110 @@
+// Attention over pages: the plan on the device, and where the parts of rows whose keys are split lie in the workspace.
+//
+// Work is two rows of tiles, one behind another, that are cut into equal stretches, one per CTA:
+//   narrow  the keys a sequence reads by itself, [pfx, len): chunks of 16 (token, query head) rows of one kv head, tiles of
+//           64 keys; per kv head sum over sequences of chunks x tiles.
+//   wide    the prefixes that groups of neighbours share, [0, pfx): chunks of up to 256 rows of the group, tiles of 128 keys
+//           that count 2 where a chunk has more than 128 rows (both halves multiply) and 1 else (the halves take keys in turn).
+// A CTA's stretch of a chunk is a part; parts of a chunk have the running maximum, the sum and the unnormalised result of
+// their keys, and lie at (number of the chunk + number of the CTA): either grows by one from part to part.
+#pragma once
+#include "pages.cuh"
+
+constexpr int NARROW_ROWS = 16, NARROW_KEYS = 64;
+constexpr int WIDE_ROWS = 256, WIDE_KEYS = 128;
+constexpr int ATTEND_MAX_SEQS = 4096;
+
+struct AttendHead {        // one per plan, on the device
+  int32_t n_seqs, n_groups;
+  int32_t narrow_tiles, narrow_chunks, narrow_each;   // per kv head; tiles per CTA
+  int32_t wide_cost, wide_chunks, wide_each;          // per kv head; cost per CTA (at least 2)
+  int32_t made_for[5];                                // sizes the layout follows from, and a mark: see plan_fits
+};
+constexpr int ATTEND_MARK = 0x41534c50;
+struct __align__(16) AttendSeq {
+  int32_t tok0, ntok, slot, len;       // ntok 0: padding
+  int32_t pfx, tile0, chunk0, group;   // shared tokens read by the group; narrow tiles and chunks before
+};
+struct __align__(16) AttendGroup {
+  int32_t tok0, ntok, slot, pfx;
+  int32_t cost0, chunk0, pad0, pad1;   // wide cost and chunks before
+};
+struct __align__(16) AttendStart { int32_t h, item, chunk, tile; };   // where a CTA's stretch begins (h < 0: it has none)
+
+struct AttendLayout {      // byte offsets in the workspace
+  size_t head, seqs, groups, same, tok_seq, narrow_start, wide_start, narrow_ml, narrow_o, wide_ml, wide_o, total;
+  int32_t narrow_grid, wide_grid;
+};
+
+struct AttendPtrs {
+  AttendHead* head;
+  AttendSeq* seqs;
+  AttendGroup* groups;
+  int32_t* same;           // [n_seqs] leading pages that an entry has in common with the one before
+  int32_t* tok_seq;        // [n_tokens] entry of a token, -1: nobody's
+  AttendStart* narrow_start;
+  AttendStart* wide_start;
+  float2* narrow_ml;       // [slot][16] (maximum in powers of two, sum)
+  float* narrow_o;         // [slot][16][128]
+  float2* wide_ml;         // [slot][256]
+  float* wide_o;           // [slot][256][128]
+};
+
+struct AttendArgs {
+  PagePool g;
+  AttendPtrs w;
+  const __nv_bfloat16* q;
+  int64_t qs_t, qs_h;      // element strides
+  __nv_bfloat16* out;
+  float* lse;              // or null
+  const float* k_scale;    // [H_k] of the layer, or null
+  int32_t* err;            // the context's word of bounded waits
+  int32_t n_q_heads, group_heads, n_tokens, n_seqs;
+  float scale_log2;
+};
+
+// Chunks of a group's rows: as many tokens as fill 256 rows, dealt out evenly.
+#ifdef __CUDACC__
+__host__
+__device__
+#endif
+inline int wide_tokens(int G) { return WIDE_ROWS / G; }
+
+#ifdef __CUDACC__
+// A workspace that holds no plan, or one for other sizes, is refused before anything is read through it.
+__device__ __forceinline__ bool plan_fits(const AttendArgs& a) {
+  const int32_t* m = a.w.head->made_for;
+  const bool fits = __ldcg(m) == ATTEND_MARK && __ldcg(m + 1) == a.n_seqs && __ldcg(m + 2) == a.n_tokens &&
+                    __ldcg(m + 3) == a.n_q_heads && __ldcg(m + 4) == a.g.n_kv_heads;
+  if (!fits && threadIdx.x == 0) note_error(a.g.err, ASL_ERR_WORKSPACE, -1);
+  return fits;
+}
+// cost of a tile of the chunk that begins at token `t` of its group
+__device__ __forceinline__ int wide_weight(const AttendGroup& gr, int chunk, int G) {
+  const int T = wide_tokens(G), n = min(T, gr.ntok - chunk * T);
+  return n * G > WIDE_ROWS / 2 ? 2 : 1;
+}
+__device__ __forceinline__ int wide_group_cost(int ntok, int pfx, int G) {      // of all its chunks
+  const int T = wide_tokens(G), tiles = (pfx + WIDE_KEYS - 1) / WIDE_KEYS;
+  const int whole = ntok / T, rest = ntok % T;
+  const int w = T * G > WIDE_ROWS / 2 ? 2 : 1;
+  return tiles * (whole * w + (rest ? (rest * G > WIDE_ROWS / 2 ? 2 : 1) : 0));
+}
+__device__ __forceinline__ AttendSeq load_seq(const AttendSeq* s) {
+  AttendSeq r;
+  reinterpret_cast<int4*>(&r)[0] = __ldcg(reinterpret_cast<const int4*>(s));
+  reinterpret_cast<int4*>(&r)[1] = __ldcg(reinterpret_cast<const int4*>(s) + 1);
+  return r;
+}
+__device__ __forceinline__ AttendGroup load_group(const AttendGroup* s) {
+  AttendGroup r;
+  reinterpret_cast<int4*>(&r)[0] = __ldcg(reinterpret_cast<const int4*>(s));
+  reinterpret_cast<int4*>(&r)[1] = __ldcg(reinterpret_cast<const int4*>(s) + 1);
+  return r;
+}
+__device__ __forceinline__ int narrow_tiles_of(const AttendSeq& s) { return max(1, (s.len - s.pfx + NARROW_KEYS - 1) / NARROW_KEYS); }
+__device__ __forceinline__ int narrow_chunks_of(int ntok, int G) { return (ntok * G + NARROW_ROWS - 1) / NARROW_ROWS; }
+#endif
+
+asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, int layer, const AttendArgs& a, int grid, cudaStream_t st);
+asl_status asl_launch_attend_wide(asl_ctx* c, const asl_pages* p, int layer, const AttendArgs& a, int grid, cudaStream_t st);

@@ -53,6 +53,7 @@
 #include <string.h>
 
 #include "asl_internal.cuh"
+#include "asl_ptx.cuh"
 
 namespace {
 
@@ -62,7 +63,6 @@ constexpr int THREADS = 640;                 // warp 0: TMA, 1: MMA, 2-3: partia
 constexpr int GROUPS = 4;
 constexpr unsigned long long OFFSET_READY = 1ull << 32;
 constexpr int SYNC_STRIDE = 8;               // words from one segment's counter to the next: a sector each
-constexpr unsigned long long WAIT_LIMIT_NS = 2000000000ull;   // every wait gives up after 2 s
 
 // Shared-memory layout of one CTA (offsets from the 1024-aligned base).  WIDE: a chunk of more than 128 rows.
 template <bool FP8, bool WIDE>
@@ -82,288 +82,11 @@ struct Smem {
   static constexpr int BYTES = OFFS + 2048;
   static_assert(N_BARS * 8 <= 384 && BYTES <= 232448, "shared memory budget of one CTA");
 };
-
-// ---------------------------------------------------------------- PTX wrappers
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ unsigned long long global_ns() {
-  unsigned long long now;
-  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-  return now;
-}
-// Looks once, without suspending the thread.
-__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-// Bounded wait.  `watch_abort`: also give up when another role raised the flag.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int code,
-                                          bool watch_abort, unsigned long long limit_ns = WAIT_LIMIT_NS) {
-  unsigned long long t0 = 0;
-  for (uint32_t it = 0;; ++it) {
-    if (mbar_try(bar, parity)) return true;
-    if ((it & 15u) == 15u) {
-      if (watch_abort && *abort_flag) return false;
-      const unsigned long long now = global_ns();
-      if (t0 == 0) t0 = now;
-      else if (now - t0 > limit_ns) break;
-    }
-  }
-  *abort_flag = code;
-  return false;
-}
-__device__ __forceinline__ unsigned long long ld_relaxed(const unsigned long long* p) {
-  unsigned long long v;
-  asm volatile("ld.relaxed.gpu.global.u64 %0, [%1];" : "=l"(v) : "l"(p) : "memory");
-  return v;
-}
-// Bounded wait until the 32-bit word at p equals `want` (acquire).  Lane 0 polls.
-__device__ __forceinline__ bool word_wait(const uint32_t* p, uint32_t want, volatile int* abort_flag, int code, int lane,
-                                          uint32_t nap_max, unsigned long long limit_ns = WAIT_LIMIT_NS) {
-  int gave_up = 0;
-  if (lane == 0) {
-    unsigned long long t0 = 0;
-    uint32_t nap = 64;
-    for (uint32_t it = 0;; ++it) {
-      uint32_t v;
-      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-      if (v == want) break;
-      if ((it & 7u) == 7u) {
-        const unsigned long long now = global_ns();
-        if (t0 == 0) t0 = now;
-        else if (now - t0 > limit_ns || *abort_flag) { gave_up = 1; if (!*abort_flag) *abort_flag = code; break; }
-      }
-      if (it >= 16) {                    // the first looks follow one another at once: what is waited for is about to come
-        __nanosleep(nap);
-        if (nap < nap_max) nap <<= 1;
-      }
-    }
-  }
-  return __shfl_sync(0xffffffffu, gave_up, 0) == 0;
-}
-
-// L2 eviction policies for the K stream: pass 1 asks L2 to keep what pass 2 will read again, pass 2
-// (and a launch that has only pass 2) marks what it reads as the first to go.
-__device__ __forceinline__ uint64_t l2_policy_keep() {
-  uint64_t pol;
-  asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
-  return pol;
-}
-__device__ __forceinline__ uint64_t l2_policy_stream() {
-  uint64_t pol;
-  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(pol));
-  return pol;
-}
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2,
-                                            uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1, {%3, %4, %5}], [%2], %6;" ::"r"(dst),
-      "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "l"(policy)
-      : "memory");
-}
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2,
-                                            int c3) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(
-          dst),
-      "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
-      : "memory");
-}
-
-__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2,
-                                            int c3, int c4) {
-  asm volatile(
-      "cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6, %7}], [%2];" ::"r"(
-          dst),
-      "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4)
-      : "memory");
-}
-
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-// D[tmem] (+)= A[smem] * B[smem], bf16 x bf16 -> fp32
-__device__ __forceinline__ void tc_mma(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accum)
-      : "memory");
-}
-// the same with 8-bit operands (E4M3 x E4M3 -> fp32), 32 channels per instruction
-__device__ __forceinline__ void tc_mma_f8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accum) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accum)
-      : "memory");
-}
-// 16 registers of an accumulator: issue only; they hold the data after tc_ld_wait on the same array.
-// Shape 32x32b: 16 consecutive columns of this thread's lane.
-__device__ __forceinline__ void tc_ld_lane(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
-// Shape 16x256b: 16 lanes x 32 columns; registers 4i..4i+3 of thread t hold columns 8i + 2(t%4) + {0, 1} of lanes
-// t/4 and t/4 + 8.
-__device__ __forceinline__ void tc_ld_quad(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
-// Waits for every tcgen05.ld this thread has issued.  The array is an in/out
-// operand so that no use of its registers can be scheduled above the wait.
-__device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[16]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
-                 "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
-               :
-               : "memory");
-}
-__device__ __forceinline__ bool elect_one() {
-  uint32_t e;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
-  return e != 0;
-}
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-__device__ __forceinline__ void bar_sync(int id, int count) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
-}
-
-// ---- two fp32 values in one 64-bit register: the FMA pipe takes fma on such pairs as
-//      one instruction, which halves the issue slots of the softmax arithmetic ----
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pk(float lo, float hi) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ f32x2 pku(uint32_t lo, uint32_t hi) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
-  return r;
-}
-__device__ __forceinline__ void upk(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ void upku(f32x2 v, uint32_t& lo, uint32_t& hi) { asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(v)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
-__device__ __forceinline__ float hsum(f32x2 v) {
-  float lo, hi;
-  upk(v, lo, hi);
-  return lo + hi;
-}
-// 2^x of a pair on the MUFU unit
-__device__ __forceinline__ f32x2 ex2_pair_mufu(f32x2 x) {
-  float a, b;
-  upk(x, a, b);
-  return pk(ex2(a), ex2(b));
-}
-// 2^x of a pair on the FMA pipe: clamp at -125, round to the nearest
-// integer n with the 1.5*2^23 trick, degree-4 minimax polynomial of 2^f on
-// f = x - n in [-0.5, 0.5] (relative error 2.6e-6), n added into the exponent field.
-// Packed additions are written as such, not as fma(a, 1, b): as fast, and six constant registers fewer.
-// ABOVE: x may lie above the fp32 range, and then comes out as infinity or NaN, as a sum that looks for an overflow
-// needs it: n = 129 fills the exponent field.  Without the upper clamp n runs into the sign bit there (2^130 as
-// -1.2e-38, 2^300 as -1.8e13).  Pass 2 has no such x: a logit is not above the log2 of its row's softmax denominator.
-// (The two more instructions a pair: eight layers of 32K tokens 466 -> 470 us, 0.9 to 1.5 % over the runs, four of 128K
-// 820 -> 821, 0.2 to 0.7 %, two prompts with W = 24 31.2 -> 31.7.  Tried: the largest x kept by one three-way maximum a pair, 1.3 to 1.5 and 0.7 to 1.9 %; 2 or 1
-// of 16 pairs polynomial in pass 1, 1.8 and 1.5 to 2.5 %.)
-template <bool ABOVE>
-__device__ __forceinline__ f32x2 ex2_pair_poly(f32x2 x) {
-  float a, b;
-  upk(x, a, b);
-  if (ABOVE) { a = fminf(a, 129.0f); b = fminf(b, 129.0f); }
-  const f32x2 xc = pk(fmaxf(a, -125.0f), fmaxf(b, -125.0f));
-  const f32x2 magic = pk(12582912.0f, 12582912.0f);
-  const f32x2 t = add2(xc, magic);
-  const f32x2 f = sub2(xc, sub2(t, magic));
-  f32x2 p = fma2(pk(0.00956967473f, 0.00956967473f), f, pk(0.0559182465f, 0.0559182465f));
-  p = fma2(p, f, pk(0.240247667f, 0.240247667f));
-  p = fma2(p, f, pk(0.693121731f, 0.693121731f));
-  p = fma2(p, f, pk(0.999999225f, 0.999999225f));
-  uint32_t tl, th, pl, ph;
-  upku(t, tl, th);
-  upku(p, pl, ph);
-  return pku(pl + (tl << 23), ph + (th << 23));
-}
 // Which of every 16 column pairs take the polynomial, spread out.  3: the loop alone is shortest at 5 (clk per tile,
 // pass 1 / pass 2, at 4, 5, 6: 1821 / 1833, 1725 / 1794, 1747 / 1839), but a polynomial takes more
 // registers; in the kernel, at 128K tokens: 155.4, 156.9, 160.9 us at 3, 4, 5.
 constexpr int POLY_OF_16 = 3;
 __device__ __forceinline__ constexpr bool pair_is_poly(int i) { return ((i & 15) * POLY_OF_16) % 16 + POLY_OF_16 >= 16; }
-
-// K-major, 128B-swizzled operand: rows of 128 B, 8-row groups 1024 B apart.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)64 << 32) | ((uint64_t)1 << 46) |
-         ((uint64_t)2 << 61);
-}
-// kind::f16, A = B = bf16, D = fp32, both operands K-major
-__device__ __forceinline__ uint32_t instr_desc(int M, int N) {
-  return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-// kind::f8f6f4, A = B = E4M3 (format code 0), D = fp32, both operands K-major
-__device__ __forceinline__ uint32_t instr_desc_f8(int M, int N) {
-  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-
 
 struct TcWork {
   const TcRun* runs;
@@ -1146,7 +869,9 @@ EncodeTiledFn encode_fn() {
   return fn;
 }
 
-bool make_map(CUtensorMap* tm, CUtensorMapDataType dtype, const void* base, int rank, const cuuint64_t* dims,
+}  // namespace
+
+bool asl_make_map(CUtensorMap* tm, CUtensorMapDataType dtype, const void* base, int rank, const cuuint64_t* dims,
               const cuuint64_t* strides_bytes, const cuuint32_t* box) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
@@ -1155,6 +880,8 @@ bool make_map(CUtensorMap* tm, CUtensorMapDataType dtype, const void* base, int 
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+
+namespace {
 
 struct ScoreKernel {
   void (*fn)(CUtensorMap, CUtensorMap, TcArgs);
@@ -1496,20 +1223,20 @@ asl_status asl_launch_score_tc(asl_ctx* c, const void* q, const void* k, const f
     const cuuint64_t qdims[5] = {128, (cuuint64_t)W, (cuuint64_t)p.n_q_heads, (cuuint64_t)p.batch, 2};
     const cuuint64_t qstr[4] = {128, (cuuint64_t)W * 128, (cuuint64_t)p.n_q_heads * W * 128, (cuuint64_t)total};
     const cuuint32_t qbox[5] = {128, box_t, box_h, 1, 1};
-    if (!make_map(&tm_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, q8, 5, qdims, qstr, qbox)) return ASL_ERR_CUDA;
+    if (!asl_make_map(&tm_q, CU_TENSOR_MAP_DATA_TYPE_UINT8, q8, 5, qdims, qstr, qbox)) return ASL_ERR_CUDA;
     const cuuint64_t kdims[3] = {128, (cuuint64_t)p.n_kv_heads, (cuuint64_t)c->sum_tokens};
     const cuuint64_t kstr[2] = {(cuuint64_t)p.k_stride[1], (cuuint64_t)p.k_stride[0]};
     const cuuint32_t kbox[3] = {128, 1, (cuuint32_t)KT};
-    if (!make_map(&tm_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, k, 3, kdims, kstr, kbox)) return ASL_ERR_CUDA;
+    if (!asl_make_map(&tm_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, k, 3, kdims, kstr, kbox)) return ASL_ERR_CUDA;
   } else {
     const cuuint64_t dims[4] = {128, (cuuint64_t)W, (cuuint64_t)p.n_q_heads, (cuuint64_t)p.batch};
     const cuuint64_t strides[3] = {(cuuint64_t)p.q_stride[2] * 2, (cuuint64_t)p.q_stride[1] * 2, (cuuint64_t)p.q_stride[0] * 2};
     const cuuint32_t box[4] = {64, box_t, box_h, 1};
-    if (!make_map(&tm_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q, 4, dims, strides, box)) return ASL_ERR_CUDA;
+    if (!asl_make_map(&tm_q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q, 4, dims, strides, box)) return ASL_ERR_CUDA;
     const cuuint64_t kdims[3] = {128, (cuuint64_t)p.n_kv_heads, (cuuint64_t)c->sum_tokens};
     const cuuint64_t kstr[2] = {(cuuint64_t)p.k_stride[1] * 2, (cuuint64_t)p.k_stride[0] * 2};
     const cuuint32_t kbox[3] = {64, 1, (cuuint32_t)KT};
-    if (!make_map(&tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, k, 3, kdims, kstr, kbox)) return ASL_ERR_CUDA;
+    if (!asl_make_map(&tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, k, 3, kdims, kstr, kbox)) return ASL_ERR_CUDA;
   }
   TcArgs a{};
   const TcList& list = tp.lists[beside][lse != nullptr];
