@@ -222,8 +222,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       s.chunk = min(x / (nt * w), whole);
       x -= s.chunk * nt * w;
       const int wl = s.chunk < whole ? w : (tokens % T) * G > WIDE_ROWS / 2 ? 2 : 1;
-      s.tile = (x + wl - 1) / wl;                               // the first tile that begins in the stretch
-      if (s.tile >= nt) s.h = -2;                               // begins with the chunk after: see wide_begin
+      s.tile = (x + wl - 1) / wl;                               // the first tile that begins in the stretch; may be the chunk's end
     }
     a.w.wide_start[k] = s;
   }
@@ -406,7 +405,7 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   a.w = ptrs_of(l, workspace);
   a.G = n_q_heads / p->n_kv_heads;
   a.n_q_heads = n_q_heads;
-  a.share = 0 && share && b->n_seqs > 1;
+  a.share = share && b->n_seqs > 1;
   a.narrow_grid = l.narrow_grid;
   a.wide_grid = l.wide_grid;
   const size_t smem = sizeof(int32_t) * (7 * (size_t)b->n_seqs + 2);
@@ -429,7 +428,7 @@ asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_b
   if (!asl_on_device(c)) return ASL_ERR_INVALID;
   if (layer < 0 || layer >= p->n_layers || !q || !out || !q_stride || !asl_aligned16(q) || !asl_aligned16(out)) return ASL_ERR_INVALID;
   for (int i = 0; i < 2; ++i)
-    if (q_stride[i] < 0 || q_stride[i] % 8) return ASL_ERR_INVALID;
+    if (q_stride[i] < p->head_dim || q_stride[i] % 8) return ASL_ERR_INVALID;
   const AttendLayout l = layout_of(c->sm_count, p->n_kv_heads, b->n_seqs, b->n_tokens, n_q_heads);
   if (!workspace || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ASL_ERR_WORKSPACE;
   if (b->n_tokens == 0) return ASL_OK;
@@ -449,7 +448,12 @@ asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_b
   a.n_tokens = b->n_tokens;
   a.n_seqs = b->n_seqs;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p->head_dim));
-  s = asl_launch_attend_narrow(c, p, layer, a, l.narrow_grid, st);
+  const bool wide = b->n_seqs > 1;       // neighbours may share (the plan says whether they do)
+  if (wide) {
+    s = asl_launch_attend_wide(c, p, a, l.wide_grid, st);
+    if (s != ASL_OK) return s;
+  }
+  s = asl_launch_attend_narrow(c, p, a, l.narrow_grid, wide, st);
   if (s != ASL_OK) return s;
   launch_after(attend_join_kernel, dim3((unsigned)(((int64_t)b->n_tokens * n_q_heads + 3) / 4)), dim3(128), st, a);
   c->launches += 1;

@@ -104,7 +104,23 @@ __device__ __forceinline__ AttendGroup load_group(const AttendGroup* s) {
 }
 __device__ __forceinline__ int narrow_tiles_of(const AttendSeq& s) { return max(1, (s.len - s.pfx + NARROW_KEYS - 1) / NARROW_KEYS); }
 __device__ __forceinline__ int narrow_chunks_of(int ntok, int G) { return (ntok * G + NARROW_ROWS - 1) / NARROW_ROWS; }
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+// Two E4M3 codes (the lower 16 bits) as bf16, exactly: bits moved into place, then times 2^(127-7), which also makes the
+// subnormal codes' values; a NaN code (0x7f, 0xff) comes out as 480, the value its bits would have, and is not in a cache.
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
+  const uint32_t w = __byte_perm(two, 0, 0x1404);                         // codes in the upper bytes of the halves
+  const uint32_t b = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 4);
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(b), "r"(0x7b807b80u), "r"(0x80008000u));   // x 2^120 (+ -0)
+  return r;
+}
+
 #endif
 
-asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, int layer, const AttendArgs& a, int grid, cudaStream_t st);
-asl_status asl_launch_attend_wide(asl_ctx* c, const asl_pages* p, int layer, const AttendArgs& a, int grid, cudaStream_t st);
+// `beside`: right behind the prefixes' kernel, whose end it does not wait for
+asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, const AttendArgs& a, int grid, bool beside, cudaStream_t st);
+asl_status asl_launch_attend_wide(asl_ctx* c, const asl_pages* p, const AttendArgs& a, int grid, cudaStream_t st);

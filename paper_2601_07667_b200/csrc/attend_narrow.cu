@@ -38,21 +38,6 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
-}
-// Two E4M3 codes (the lower 16 bits) as bf16, exactly: bits moved into place, then times 2^(127-7), which also makes the
-// subnormal codes' values; a NaN code (0x7f, 0xff) comes out as 480, the value its bits would have, and is not in a cache.
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
-  const uint32_t w = __byte_perm(two, 0, 0x1404);                         // codes in the upper bytes of the halves
-  const uint32_t b = (w & 0x80008000u) | ((w & 0x7f007f00u) >> 4);
-  uint32_t r;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(b), "r"(0x7b807b80u), "r"(0x80008000u));   // x 2^120 (+ -0)
-  return r;
-}
-
 // A CTA's stretch: its chunks one after another.
 struct Walk {
   int h, i, chunk, tile, left;
@@ -93,7 +78,7 @@ struct Walk {
 
 template <bool FP8>
 __global__ void __launch_bounds__(WARPS * 32 + 32, 2)
-attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, AttendArgs a) {
+attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, AttendArgs a, int beside) {
   using S = NarrowSmem<FP8>;
   extern __shared__ uint8_t raw[];
   uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -108,7 +93,9 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  pdl_wait_predecessor();
+  // Behind the prefixes' kernel (`beside`) nothing is waited for: that kernel lets this one start only when all before it is
+  // done, and neither writes what the other reads.
+  if (!beside) pdl_wait_predecessor();
   Walk w;
   const int n_kv = a.g.n_kv_heads;
   const bool any = plan_fits(a) && w.begin(a, n_kv);
@@ -366,11 +353,12 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   }
   __syncthreads();
   if (threadIdx.x == 0 && *s_abort) atomicCAS(a.err, 0, *s_abort);
+  if (beside) pdl_wait_predecessor();                  // the end of this kernel is the end of all before it
 }
 
 }  // namespace
 
-asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, int layer, const AttendArgs& a, int grid, cudaStream_t st) {
+asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, const AttendArgs& a, int grid, bool beside, cudaStream_t st) {
   const bool fp8 = p->k_dtype == ASL_K_FP8_E4M3;
   const cuuint64_t n_rows = (cuuint64_t)p->n_pages * p->n_kv_heads * p->page_size;
   const cuuint32_t piece = p->page_size < NARROW_KEYS ? p->page_size : NARROW_KEYS;
@@ -383,7 +371,7 @@ asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, int layer, c
   auto kernel = fp8 ? attend_narrow_kernel<true> : attend_narrow_kernel<false>;
   const int smem = fp8 ? NarrowSmem<true>::BYTES : NarrowSmem<false>::BYTES;
   ASL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  launch_after_smem(kernel, dim3(grid), dim3(WARPS * 32 + 32), smem, st, tm_k, tm_v, a);
+  launch_after_smem(kernel, dim3(grid), dim3(WARPS * 32 + 32), smem, st, tm_k, tm_v, a, beside);
   c->launches += 1;
   ASL_CUDA(cudaGetLastError());
   return ASL_OK;
