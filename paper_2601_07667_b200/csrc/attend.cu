@@ -13,28 +13,38 @@ constexpr int NARROW_CTAS = 2;             // per SM
 constexpr int SHARE_MIN_KEYS = 1024;
 
 // Leading pages that an entry of the batch has in common with the one before it; only pages that both hold in full.
-__global__ void __launch_bounds__(128) attend_same_kernel(PagePool g, asl_batch b, int32_t* same) {
+constexpr int SAME_THREADS = 256, SAME_EACH = 8;
+__global__ void __launch_bounds__(SAME_THREADS) attend_same_kernel(PagePool g, asl_batch b, int32_t* same) {
+  __shared__ int first[SAME_THREADS / 32];
   pdl_wait_predecessor();
-  const int i = blockIdx.x;
+  const int i = blockIdx.x, tid = threadIdx.x;
   int m = 0;
   if (i > 0) {
     const int s = __ldcg(b.slots + i), r = __ldcg(b.slots + i - 1);
     if ((unsigned)s < (unsigned)g.max_seqs && (unsigned)r < (unsigned)g.max_seqs)
-      m = min(min(__ldcg(g.len + s), __ldcg(g.len + r)) >> g.page_shift, g.max_pages);
+      m = max(0, min(min(__ldcg(g.len + s), __ldcg(g.len + r)) >> g.page_shift, g.max_pages));
     const int32_t* x = g.table + (int64_t)s * g.max_pages;
     const int32_t* y = g.table + (int64_t)r * g.max_pages;
-    for (int j0 = 0; j0 < m; j0 += 128) {
-      const int j = j0 + threadIdx.x;
-      const bool differs = j < m && __ldcg(x + j) != __ldcg(y + j);
-      const unsigned any = __ballot_sync(0xffffffffu, differs);
-      __shared__ int first[4];
-      if ((threadIdx.x & 31) == 0) first[threadIdx.x >> 5] = any ? j0 + threadIdx.x + __ffs(any) - 1 : m;
+    for (int j0 = 0; j0 < m; j0 += SAME_THREADS * SAME_EACH) {
+      int u[SAME_EACH], v[SAME_EACH], at = m;
+#pragma unroll
+      for (int q = 0; q < SAME_EACH; ++q) {
+        const int j = j0 + q * SAME_THREADS + tid;
+        u[q] = j < m ? __ldcg(x + j) : 0;
+        v[q] = j < m ? __ldcg(y + j) : 0;
+      }
+#pragma unroll
+      for (int q = SAME_EACH - 1; q >= 0; --q)
+        if (u[q] != v[q]) at = j0 + q * SAME_THREADS + tid;
+      at = __reduce_min_sync(0xffffffffu, at);
+      if ((tid & 31) == 0) first[tid >> 5] = at;
       __syncthreads();
-      m = min(m, min(min(first[0], first[1]), min(first[2], first[3])));
+#pragma unroll
+      for (int q = 0; q < SAME_THREADS / 32; ++q) m = min(m, first[q]);
       __syncthreads();
     }
   }
-  if (threadIdx.x == 0) same[i] = max(m, 0);
+  if (tid == 0) same[i] = m;
 }
 
 __device__ __forceinline__ int scan_step(int v, int* part, int& total) {       // as block_scan, 512 threads
@@ -67,56 +77,76 @@ struct PlanArgs {
 
 // One block: groups of neighbours, prefix sums over sequences and groups, and where every CTA's stretch begins.
 __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
-  extern __shared__ int32_t sm[];          // per sequence: ntok, len, group, then first narrow tile (one more at the end)
+  extern __shared__ int32_t sm[];
   __shared__ int part[PLAN_THREADS / 32];
-  __shared__ int n_groups_s, bad;
+  __shared__ int n_groups_s;
+  __shared__ unsigned long long most_s;
   pdl_wait_predecessor();
   const int tid = threadIdx.x, n = a.b.n_seqs, G = a.G;
   int32_t* ntok = sm;
   int32_t* len = sm + n;
   int32_t* grp = sm + 2 * n;
-  int32_t* first = sm + 3 * n;             // [n + 1]
+  int32_t* first = sm + 3 * n;             // [n + 1] narrow tiles before; until the groups are known: tokens in common
   int32_t* gpfx = first + n + 1;           // per group: shared tokens, first entry, wide cost before
   int32_t* gat = gpfx + n;
   int32_t* gcost = gat + n;                // [n + 1]
-  if (tid == 0) a.w.head->made_for[0] = 0;
-  for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tok_seq[t] = -1;
+  if (tid == 0) { a.w.head->made_for[0] = 0; most_s = 0; }
+  __syncthreads();
+  for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tok_seq[t] = make_int2(-1, -1);
   for (int i = tid; i < n; i += PLAN_THREADS) {
     const int s = __ldcg(a.b.slots + i), t0 = __ldcg(a.b.cu_q + i), t1 = __ldcg(a.b.cu_q + i + 1);
     const bool slot_ok = (unsigned)s < (unsigned)a.g.max_seqs, tok_ok = t0 >= 0 && t1 >= t0 && t1 <= a.b.n_tokens;
     if (slot_ok && !tok_ok) note_error(a.g.err, ASL_ERR_INVALID, s);
     ntok[i] = slot_ok && tok_ok ? t1 - t0 : 0;
     len[i] = ntok[i] ? min(max(__ldcg(a.g.len + s), 0), a.g.max_pages << a.g.page_shift) : 0;
+    first[i] = a.share ? __ldcg(a.w.same + i) << a.g.page_shift : 0;
+    // tiles, were nothing shared: they are counted in 32 bits
+    if (ntok[i]) atomicAdd(&most_s, (unsigned long long)narrow_chunks_of(ntok[i], G) * (unsigned)(len[i] / NARROW_KEYS + 2));
   }
   __syncthreads();
-  // Groups: an entry joins the group before it where that group then saves no less than without it.
-  if (tid == 0) {
-    int ng = 0, held = 0, keys = 0;                          // of the open group: entries, and its shared tokens
-    int64_t most = 0;                                        // tiles, were nothing shared: they are counted in 32 bits
-    bool open = false;
-    for (int i = 0; i < n; ++i) {
-      if (ntok[i] == 0) { grp[i] = -1; open = false; continue; }
-      most += (int64_t)narrow_chunks_of(ntok[i], G) * (len[i] / NARROW_KEYS + 2);
-      const int own = max(0, len[i] - ntok[i]) >> a.g.page_shift << a.g.page_shift;     // all its tokens see these
-      const int both = open && a.share ? min(min(keys, own), __ldcg(a.w.same + i) << a.g.page_shift) : 0;
-      if (both > 0 && (int64_t)held * both >= (int64_t)(held - 1) * keys) {
-        keys = both;
-        ++held;
-      } else {
-        gat[ng++] = i;
-        held = 1;
-        keys = own;
-        open = true;
+  if (most_s >= 1ull << 30) {
+    if (tid == 0) note_error(a.g.err, ASL_ERR_UNSUPPORTED, -1);
+    return;
+  }
+  // Groups: an entry joins the group before it where that group then saves no less than without it.  One warp, 32 entries in
+  // its lanes, all of whose threads walk them together.
+  if (tid < 32) {
+    int ng = 0, held = 0, keys = 0;                          // of the open group: entries (0: none is open), shared tokens
+    auto close = [&]() { if (held && tid == 0) gpfx[ng - 1] = held > 1 && (int64_t)(held - 1) * keys >= SHARE_MIN_KEYS ? keys : 0; };
+    for (int i0 = 0; i0 < n; i0 += 32) {
+      const int i = i0 + tid;
+      int mine = 0, own = 0, com = 0, group = -1;
+      if (i < n) {
+        mine = ntok[i];
+        own = max(0, len[i] - ntok[i]) >> a.g.page_shift << a.g.page_shift;        // all its tokens see these
+        com = min(own, first[i]);
       }
-      grp[i] = ng - 1;
-      gpfx[ng - 1] = held > 1 && (int64_t)(held - 1) * keys >= SHARE_MIN_KEYS ? keys : 0;
+      for (int j = 0; j < min(32, n - i0); ++j) {
+        const int has = __shfl_sync(0xffffffffu, mine, j), o = __shfl_sync(0xffffffffu, own, j), c = __shfl_sync(0xffffffffu, com, j);
+        if (!has) {
+          close();
+          held = 0;
+          continue;
+        }
+        const int both = min(keys, c);
+        if (held && both > 0 && (int64_t)held * both >= (int64_t)(held - 1) * keys) {
+          keys = both;
+          ++held;
+        } else {
+          close();
+          if (tid == 0) gat[ng] = i0 + j;
+          ++ng;
+          held = 1;
+          keys = o;
+        }
+        if (tid == j) group = ng - 1;
+      }
+      if (i < n) grp[i] = group;
     }
-    n_groups_s = ng;
-    bad = most >= 1 << 30;
-    if (bad) note_error(a.g.err, ASL_ERR_UNSUPPORTED, -1);
+    close();
+    if (tid == 0) n_groups_s = ng;
   }
   __syncthreads();
-  if (bad) return;
   const int ng = n_groups_s;
   int tiles = 0, chunks = 0;
   for (int i0 = 0; i0 < n; i0 += PLAN_THREADS) {
@@ -141,7 +171,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       s.chunk0 = c0;
       s.group = grp[i];
       a.w.seqs[i] = s;
-      for (int t = 0; t < ntok[i]; ++t) a.w.tok_seq[s.tok0 + t] = i;
+      for (int t = 0; t < ntok[i]; ++t) a.w.tok_seq[s.tok0 + t] = make_int2(i, grp[i]);
     }
     tiles += tsum;
     chunks += csum;
@@ -180,10 +210,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   if (tid == 0) { first[n] = tiles; gcost[ng] = cost; }
   __syncthreads();
   const int H = a.g.n_kv_heads;
-  const int narrow_each = (int)(((int64_t)H * tiles + a.narrow_grid - 1) / a.narrow_grid);
+  const int narrow_each = max(1, (int)(((int64_t)H * tiles + a.narrow_grid - 1) / a.narrow_grid));
   const int wide_each = max(2, (int)(((int64_t)H * cost + a.wide_grid - 1) / a.wide_grid));
   for (int k = tid; k < a.narrow_grid; k += PLAN_THREADS) {
-    AttendStart s = {-1, 0, 0, 0};
+    AttendStart s = {};
+    s.h = -1;
+    s.items = n; s.total = tiles; s.chunks = chunks; s.each = narrow_each;
     const int64_t u = (int64_t)k * narrow_each;
     if (u < (int64_t)H * tiles) {
       s.h = (int)(u / tiles);
@@ -197,11 +229,14 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       const int nt = max(1, (len[lo] - gpfx[grp[lo]] + NARROW_KEYS - 1) / NARROW_KEYS);
       s.chunk = (r - first[lo]) / nt;
       s.tile = (r - first[lo]) % nt;
+      s.seq = a.w.seqs[lo];
     }
     a.w.narrow_start[k] = s;
   }
   for (int k = tid; k < a.wide_grid; k += PLAN_THREADS) {
-    AttendStart s = {-1, 0, 0, 0};
+    AttendStart s = {};
+    s.h = -1;
+    s.items = ng; s.total = cost; s.chunks = wchunks; s.each = wide_each;
     const int64_t u = (int64_t)k * wide_each;
     if (u < (int64_t)H * cost) {
       s.h = (int)(u / cost);
@@ -214,14 +249,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       s.item = lo;
       const int nt = (gpfx[lo] + WIDE_KEYS - 1) / WIDE_KEYS, T = wide_tokens(G), w = T * G > WIDE_ROWS / 2 ? 2 : 1;
       int x = r - gcost[lo];
-      // full chunks first; the last one may count less
-      const int last = lo + 1 < ng ? gat[lo + 1] : n;
-      int e = last;
-      while (e > gat[lo] + 1 && ntok[e - 1] == 0) --e;
-      const int tokens = __ldcg(a.b.cu_q + e - 1) + ntok[e - 1] - __ldcg(a.b.cu_q + gat[lo]), whole = tokens / T;
+      s.group = a.w.groups[lo];
+      const int whole = s.group.ntok / T;                       // full chunks first; the last one may count less
       s.chunk = min(x / (nt * w), whole);
       x -= s.chunk * nt * w;
-      const int wl = s.chunk < whole ? w : (tokens % T) * G > WIDE_ROWS / 2 ? 2 : 1;
+      const int wl = s.chunk < whole ? w : s.group.ntok % T * G > WIDE_ROWS / 2 ? 2 : 1;
       s.tile = (x + wl - 1) / wl;                               // the first tile that begins in the stretch; may be the chunk's end
     }
     a.w.wide_start[k] = s;
@@ -233,7 +265,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     h->n_groups = ng;
     h->narrow_tiles = tiles;
     h->narrow_chunks = chunks;
-    h->narrow_each = max(1, narrow_each);
+    h->narrow_each = narrow_each;
     h->wide_cost = cost;
     h->wide_chunks = wchunks;
     h->wide_each = wide_each;
@@ -245,82 +277,98 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   }
 }
 
-// Rows whose keys were split: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m the largest m_i, and the same for lse.  A
-// warp a row, four channels a lane; parts in a fixed order, so that a row comes out the same on every run.
+// Rows whose keys were split: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m the largest m_i, and the same for lse.
+// WARPS warps a row, four channels a lane, up to eight parts in flight each; parts in a fixed order, so that a row comes out the
+// same on every run.  A chain of four round trips (token, sequence and group, parts, result) bounds it where rows are few.
+template <int WARPS>
 __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
+  __shared__ float4 joined[4][32];
   pdl_wait_predecessor();
-  if (!plan_fits(a)) return;
-  const int lane = threadIdx.x & 31;
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 5);
-  if (row >= a.n_tokens * a.n_q_heads) return;
-  const int t = row / a.n_q_heads, head = row % a.n_q_heads, G = a.group_heads, h = head / G, g = head % G;
-  const int i = __ldcg(a.w.tok_seq + t);
-  if (i < 0) return;
-  const AttendSeq s = load_seq(a.w.seqs + i);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = WARPS == 1 ? 0 : warp;
+  const int row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x;
+  const bool exists = row < a.n_tokens * a.n_q_heads;
+  const int t = exists ? row / a.n_q_heads : 0, head = row - t * a.n_q_heads, G = a.group_heads, h = head / G, g = head - h * G;
+  const int2 who = __ldcg(a.w.tok_seq + t);
   const AttendHead* hd = a.w.head;
+  const int n_tiles = __ldcg(&hd->narrow_tiles), n_chunks = __ldcg(&hd->narrow_chunks), n_each = __ldcg(&hd->narrow_each);
+  const int w_cost = __ldcg(&hd->wide_cost), w_chunks = __ldcg(&hd->wide_chunks), w_each = __ldcg(&hd->wide_each);
+  if (!plan_fits(a) || !exists || who.x < 0) return;              // (the same for all warps of a row)
+  const AttendSeq s = load_seq(a.w.seqs + who.x);
+  const AttendGroup gr = load_group(a.w.groups + who.y);
   const int nt = narrow_tiles_of(s), lr = (t - s.tok0) * G + g, chunk = lr / NARROW_ROWS;
-  const int64_t each = __ldcg(&hd->narrow_each);
-  const int64_t ta = (int64_t)h * __ldcg(&hd->narrow_tiles) + s.tile0 + (int64_t)chunk * nt;
-  const int c0 = (int)(ta / each), c1 = (int)((ta + nt - 1) / each);
+  const int64_t ta = (int64_t)h * n_tiles + s.tile0 + (int64_t)chunk * nt;
+  const int c0 = (int)(ta / n_each), c1 = (int)((ta + nt - 1) / n_each);
   if (s.pfx == 0 && c0 == c1) return;                             // written where it was computed
-  const int64_t slot = (int64_t)h * __ldcg(&hd->narrow_chunks) + s.chunk0 + chunk;
   // parts: narrow ones c0 .. c1, then those of the prefix (two halves each where a chunk's rows fill one)
-  const float2* ml[2];
-  const float* o[2];
-  int count[2], step[2];
-  ml[0] = a.w.narrow_ml + (slot + c0) * NARROW_ROWS + lr % NARROW_ROWS;
-  o[0] = a.w.narrow_o + ((slot + c0) * NARROW_ROWS + lr % NARROW_ROWS) * 128;
-  count[0] = c1 - c0 + 1;
-  step[0] = NARROW_ROWS;
-  count[1] = 0;
-  ml[1] = nullptr; o[1] = nullptr; step[1] = 0;
+  const int64_t n_row = ((int64_t)h * n_chunks + s.chunk0 + chunk + c0) * NARROW_ROWS + lr % NARROW_ROWS;
+  const int n_parts = c1 - c0 + 1;
+  int64_t w_row = 0;
+  int total = n_parts, w_step = 0;
   if (s.pfx) {
-    const AttendGroup gr = load_group(a.w.groups + s.group);
-    const int T = wide_tokens(G), ch = (t - gr.tok0) / T, wr = (t - gr.tok0) % T * G + g;
+    const int T = wide_tokens(G), ch = (t - gr.tok0) / T, wr = ((t - gr.tok0) - ch * T) * G + g;
     const int wt = (gr.pfx + WIDE_KEYS - 1) / WIDE_KEYS, w = wide_weight(gr, ch, G), w0 = T * G > WIDE_ROWS / 2 ? 2 : 1;
-    const int64_t we = __ldcg(&hd->wide_each);
-    const int64_t a0 = (int64_t)h * __ldcg(&hd->wide_cost) + gr.cost0 + (int64_t)ch * wt * w0;
-    const int x0 = (int)(a0 / we), x1 = (int)((a0 + (int64_t)(wt - 1) * w) / we);
-    const int64_t ws = (int64_t)h * __ldcg(&hd->wide_chunks) + gr.chunk0 + ch + x0;
+    const int64_t a0 = (int64_t)h * w_cost + gr.cost0 + (int64_t)ch * wt * w0;
+    const int x0 = (int)(a0 / w_each), x1 = (int)((a0 + (int64_t)(wt - 1) * w) / w_each);
     const int halves = w == 1 ? 2 : 1;
-    step[1] = WIDE_ROWS / halves;
-    count[1] = (x1 - x0 + 1) * halves;
-    ml[1] = a.w.wide_ml + ws * WIDE_ROWS + wr;
-    o[1] = a.w.wide_o + (ws * WIDE_ROWS + wr) * 128;
+    w_row = ((int64_t)h * w_chunks + gr.chunk0 + ch + x0) * WIDE_ROWS + wr;
+    w_step = WIDE_ROWS / halves;
+    total += (x1 - x0 + 1) * halves;
   }
-  const int total = count[0] + count[1];
-  auto entry = [&](int k) { return k < count[0] ? __ldcg(ml[0] + (int64_t)k * step[0]) : __ldcg(ml[1] + (int64_t)(k - count[0]) * step[1]); };
-  float top = -INFINITY;
-  for (int k = lane; k < total; k += 32) top = fmaxf(top, entry(k).x);
+  auto entry = [&](int k) {
+    if (k >= total) return make_float2(-INFINITY, 0.0f);
+    return k < n_parts ? __ldcg(a.w.narrow_ml + n_row + k * NARROW_ROWS) : __ldcg(a.w.wide_ml + w_row + (int64_t)(k - n_parts) * w_step);
+  };
+  auto result = [&](int k) {
+    const float* p = k < n_parts ? a.w.narrow_o + (n_row + k * NARROW_ROWS) * 128 : a.w.wide_o + (w_row + (int64_t)(k - n_parts) * w_step) * 128;
+    return __ldcg(reinterpret_cast<const float4*>(p) + lane);
+  };
+  float2 e = entry(lane);
+  float4 v[8];
+#pragma unroll
+  for (int q = 0; q < 8; ++q)
+    if (sub + q * WARPS < total) v[q] = result(sub + q * WARPS);
+  float top = e.x;
+  for (int k = lane + 32; k < total; k += 32) top = fmaxf(top, entry(k).x);
 #pragma unroll
   for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
   const float ref = top == -INFINITY ? 0.0f : top;
   float sum = 0.0f;
   float4 acc = make_float4(0, 0, 0, 0);
   for (int k0 = 0; k0 < total; k0 += 32) {
-    const float2 e = k0 + lane < total ? entry(k0 + lane) : make_float2(-INFINITY, 0.0f);
+    if (k0) e = entry(k0 + lane);
     const float f = ex2(e.x - ref);
     sum += e.y * f;
     const int m = min(32, total - k0);
-#pragma unroll 4
-    for (int k = 0; k < m; ++k) {
-      const float fk = __shfl_sync(0xffffffffu, f, k);
-      const float mk = __shfl_sync(0xffffffffu, e.x, k);
-      const int kk = k0 + k;
-      if (mk == -INFINITY) continue;                              // the part saw nothing: its result may be anything
-      const float* p = kk < count[0] ? o[0] + (int64_t)kk * step[0] * 128 : o[1] + (int64_t)(kk - count[0]) * step[1] * 128;
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(p) + lane);
-      acc.x += v.x * fk; acc.y += v.y * fk; acc.z += v.z * fk; acc.w += v.w * fk;
+    for (int b = 0; b < 32 && b < m; b += 8 * WARPS) {
+      if (k0 + b) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+          if (b + sub + q * WARPS < m) v[q] = result(k0 + b + sub + q * WARPS);
+      }
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const int k = b + sub + q * WARPS;
+        const float fk = __shfl_sync(0xffffffffu, f, k & 31), mk = __shfl_sync(0xffffffffu, e.x, k & 31);
+        if (k < m && mk != -INFINITY) {                           // a part that saw nothing may hold anything
+          acc.x += v[q].x * fk; acc.y += v[q].y * fk; acc.z += v[q].z * fk; acc.w += v[q].w * fk;
+        }
+      }
     }
   }
 #pragma unroll
   for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+  if (WARPS > 1) {
+    joined[warp][lane] = acc;
+    __syncthreads();
+    if (warp) return;
+#pragma unroll
+    for (int k = 1; k < WARPS; ++k) {
+      const float4 o = joined[k][lane];
+      acc.x += o.x; acc.y += o.y; acc.z += o.z; acc.w += o.w;
+    }
+  }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), hi = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-  uint2 v;
-  v.x = *reinterpret_cast<uint32_t*>(&lo);
-  v.y = *reinterpret_cast<uint32_t*>(&hi);
-  *reinterpret_cast<uint2*>(a.out + (int64_t)row * 128 + lane * 4) = v;
+  *reinterpret_cast<uint2*>(a.out + (int64_t)row * 128 + lane * 4) = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
   if (a.lse && lane == 0) a.lse[row] = (ref + log2f(sum)) * 0.6931471805599453f;
 }
 
@@ -341,7 +389,7 @@ AttendLayout layout_of(int sm_count, int n_kv_heads, int n_seqs, int n_tokens, i
   l.seqs = take(sizeof(AttendSeq) * n_seqs);
   l.groups = take(sizeof(AttendGroup) * n_seqs);
   l.same = take(sizeof(int32_t) * n_seqs);
-  l.tok_seq = take(sizeof(int32_t) * n_tokens);
+  l.tok_seq = take(sizeof(int2) * n_tokens);
   l.narrow_start = take(sizeof(AttendStart) * l.narrow_grid);
   l.wide_start = take(sizeof(AttendStart) * l.wide_grid);
   l.narrow_ml = take(sizeof(float2) * NARROW_ROWS * narrow_slots);
@@ -359,7 +407,7 @@ AttendPtrs ptrs_of(const AttendLayout& l, void* workspace) {
   p.seqs = reinterpret_cast<AttendSeq*>(w + l.seqs);
   p.groups = reinterpret_cast<AttendGroup*>(w + l.groups);
   p.same = reinterpret_cast<int32_t*>(w + l.same);
-  p.tok_seq = reinterpret_cast<int32_t*>(w + l.tok_seq);
+  p.tok_seq = reinterpret_cast<int2*>(w + l.tok_seq);
   p.narrow_start = reinterpret_cast<AttendStart*>(w + l.narrow_start);
   p.wide_start = reinterpret_cast<AttendStart*>(w + l.wide_start);
   p.narrow_ml = reinterpret_cast<float2*>(w + l.narrow_ml);
@@ -412,7 +460,7 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   if (smem > 48 * 1024)
     ASL_CUDA(cudaFuncSetAttribute(attend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (7 * ATTEND_MAX_SEQS + 2)));
   if (a.share) {
-    launch_after(attend_same_kernel, dim3(b->n_seqs), dim3(128), st, a.g, a.b, a.w.same);
+    launch_after(attend_same_kernel, dim3(b->n_seqs), dim3(SAME_THREADS), st, a.g, a.b, a.w.same);
     c->launches += 1;
   }
   launch_after_smem(attend_plan_kernel, dim3(1), dim3(PLAN_THREADS), smem, st, a);
@@ -455,7 +503,10 @@ asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_b
   }
   s = asl_launch_attend_narrow(c, p, a, l.narrow_grid, wide, st);
   if (s != ASL_OK) return s;
-  launch_after(attend_join_kernel, dim3((unsigned)(((int64_t)b->n_tokens * n_q_heads + 3) / 4)), dim3(128), st, a);
+  // four warps a row where they all find room at once, else one
+  const int64_t rows = (int64_t)b->n_tokens * n_q_heads;
+  if (rows <= 16 * c->sm_count) launch_after(attend_join_kernel<4>, dim3((unsigned)rows), dim3(128), st, a);
+  else launch_after(attend_join_kernel<1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), st, a);
   c->launches += 1;
   ASL_CUDA(cudaGetLastError());
   return ASL_OK;

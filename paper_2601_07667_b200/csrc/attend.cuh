@@ -29,7 +29,12 @@ struct __align__(16) AttendGroup {
   int32_t tok0, ntok, slot, pfx;
   int32_t cost0, chunk0, pad0, pad1;   // wide cost and chunks before
 };
-struct __align__(16) AttendStart { int32_t h, item, chunk, tile; };   // where a CTA's stretch begins (h < 0: it has none)
+// Where a CTA's stretch begins (h < 0: it has none), with all that it needs to know there: one round trip to memory.
+struct __align__(16) AttendStart {
+  int32_t h, item, chunk, tile;
+  union { AttendSeq seq; AttendGroup group; };
+  int32_t items, total, chunks, each;  // sequences or groups; tiles or cost, and chunks, per kv head; per CTA
+};
 
 struct AttendLayout {      // byte offsets in the workspace
   size_t head, seqs, groups, same, tok_seq, narrow_start, wide_start, narrow_ml, narrow_o, wide_ml, wide_o, total;
@@ -41,7 +46,7 @@ struct AttendPtrs {
   AttendSeq* seqs;
   AttendGroup* groups;
   int32_t* same;           // [n_seqs] leading pages that an entry has in common with the one before
-  int32_t* tok_seq;        // [n_tokens] entry of a token, -1: nobody's
+  int2* tok_seq;           // [n_tokens] a token's entry (-1: nobody's) and group
   AttendStart* narrow_start;
   AttendStart* wide_start;
   float2* narrow_ml;       // [slot][16] (maximum in powers of two, sum)
@@ -89,6 +94,12 @@ __device__ __forceinline__ int wide_group_cost(int ntok, int pfx, int G) {      
   const int whole = ntok / T, rest = ntok % T;
   const int w = T * G > WIDE_ROWS / 2 ? 2 : 1;
   return tiles * (whole * w + (rest ? (rest * G > WIDE_ROWS / 2 ? 2 : 1) : 0));
+}
+__device__ __forceinline__ AttendStart load_start(const AttendStart* s) {
+  AttendStart r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) reinterpret_cast<int4*>(&r)[i] = __ldcg(reinterpret_cast<const int4*>(s) + i);
+  return r;
 }
 __device__ __forceinline__ AttendSeq load_seq(const AttendSeq* s) {
   AttendSeq r;

@@ -42,38 +42,45 @@ __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uin
 struct Walk {
   int h, i, chunk, tile, left;
   AttendSeq s;
-  int nt, nch;
-  __device__ __forceinline__ void load(const AttendArgs& a) {
-    s = load_seq(a.w.seqs + i);
+  int nt, nch, items, total, chunks, each;
+  __device__ __forceinline__ void sizes(const AttendArgs& a) {
     nt = narrow_tiles_of(s);
     nch = narrow_chunks_of(s.ntok, a.group_heads);
   }
-  __device__ __forceinline__ bool begin(const AttendArgs& a, int n_kv_heads) {
-    const int4 st = __ldcg(reinterpret_cast<const int4*>(a.w.narrow_start + blockIdx.x));
-    h = st.x; i = st.y; chunk = st.z; tile = st.w;
-    if (h < 0) return false;
-    const int each = __ldcg(&a.w.head->narrow_each);
-    left = (int)min((int64_t)each, (int64_t)n_kv_heads * __ldcg(&a.w.head->narrow_tiles) - (int64_t)blockIdx.x * each);
-    load(a);
+  __device__ __forceinline__ bool begin(const AttendArgs& a) {
+    const AttendStart st = load_start(a.w.narrow_start + blockIdx.x);
+    if (!plan_fits(a) || st.h < 0) return false;
+    h = st.h; i = st.item; chunk = st.chunk; tile = st.tile;
+    s = st.seq;
+    items = st.items; total = st.total; chunks = st.chunks; each = st.each;
+    left = (int)min((int64_t)each, (int64_t)a.g.n_kv_heads * total - (int64_t)blockIdx.x * each);
+    sizes(a);
     return true;
   }
   __device__ __forceinline__ int here() const { return min(nt - tile, left); }     // tiles of this part
   // the next chunk; false at the end
-  __device__ __forceinline__ bool next(const AttendArgs& a, int n_seqs) {
+  __device__ __forceinline__ bool next(const AttendArgs& a) {
     left -= here();
     if (left <= 0) return false;
     tile = 0;
     if (++chunk < nch) return true;
     chunk = 0;
     do {
-      if (++i >= n_seqs) {
+      if (++i >= items) {
         i = 0;
         if (++h >= a.g.n_kv_heads) return false;
       }
-      load(a);
+      s = load_seq(a.w.seqs + i);
+      sizes(a);
     } while (nch == 0);
     return true;
   }
+  // A chunk whose keys nobody else has part of: its rows are written at once.
+  __device__ __forceinline__ bool sole() const {
+    const int64_t at = (int64_t)h * total + s.tile0 + (int64_t)chunk * nt;
+    return s.pfx == 0 && at / each == (at + nt - 1) / each;
+  }
+  __device__ __forceinline__ int64_t slot() const { return (int64_t)h * chunks + s.chunk0 + chunk + blockIdx.x; }
 };
 
 template <bool FP8>
@@ -98,8 +105,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   if (!beside) pdl_wait_predecessor();
   Walk w;
   const int n_kv = a.g.n_kv_heads;
-  const bool any = plan_fits(a) && w.begin(a, n_kv);
-  const int n_seqs = any ? __ldcg(&a.w.head->n_seqs) : 0;
+  const bool any = w.begin(a);
 
   if (any && warp == WARPS) {
     // ---- copies: tiles of whole pages' pieces; pages behind the sequence's end are not read ----
@@ -137,7 +143,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           }
         }
       }
-      if (more) more = w.next(a, n_seqs);
+      if (more) more = w.next(a);
     }
     if (*s_abort) {                                    // copies in flight land before the block ends
       for (int i = max(0, n - STAGES); i < n; ++i) mbar_wait(full(i % STAGES), (i / STAGES) & 1, s_abort, 202, false);
@@ -300,10 +306,8 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         ml[warp * 16 + gid] = make_float2(m[0], l[0]);
         ml[warp * 16 + gid + 8] = make_float2(m[1], l[1]);
       }
-      const int64_t each = __ldcg(&a.w.head->narrow_each);
-      const int64_t tile_a = (int64_t)w.h * __ldcg(&a.w.head->narrow_tiles) + w.s.tile0 + (int64_t)w.chunk * w.nt;
-      const bool sole = w.s.pfx == 0 && tile_a / each == (tile_a + w.nt - 1) / each;
-      const int64_t slot = (int64_t)w.h * __ldcg(&a.w.head->narrow_chunks) + w.s.chunk0 + w.chunk + blockIdx.x;
+      const bool sole = w.sole();
+      const int64_t slot = w.slot();
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (lr0 + 8 * i >= rows) break;
@@ -348,7 +352,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         }
       }
       bar_sync(1, WARPS * 32);                         // ml and join are free
-      more = w.next(a, n_seqs);
+      more = w.next(a);
     }
   }
   __syncthreads();

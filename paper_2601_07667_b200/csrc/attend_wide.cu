@@ -31,13 +31,16 @@ struct WideSmem {
   static constexpr int MISC = BARS + 256;
   static constexpr int BYTES = MISC + 16 + 1024;
   static constexpr int THREADS = FP8 ? 512 : 384;
+  // Registers a thread: a row of 128 logits stays in them.  Launched with REGS each; the warpgroups' shares are no more together.
+  static constexpr int REGS = FP8 ? 128 : 168, REGS_FEW = FP8 ? 56 : 72, REGS_ROWS = FP8 ? 200 : 216;
+  static_assert(REGS * THREADS >= REGS_FEW * (THREADS - 256) + REGS_ROWS * 256, "a warpgroup would wait for registers");
   static_assert(N_BARS * 8 <= 256 && BYTES <= 232448, "shared memory budget of one CTA");
 };
 
 // A CTA's stretch: chunk by chunk the tiles tile .. end - 1.
 struct Walk {
   int h, gi, chunk, tile, end;
-  int nt, weight, rows;
+  int nt, weight, rows, items, total, chunks;
   int64_t stop;                            // cost at which the stretch ends
   AttendGroup g;
   __device__ __forceinline__ bool set(const AttendArgs& a) {        // a chunk of group g: its tiles in the stretch
@@ -46,26 +49,25 @@ struct Walk {
     weight = wide_weight(g, chunk, a.group_heads);
     rows = min(T, g.ntok - chunk * T) * a.group_heads;
     const int w0 = T * a.group_heads > WIDE_ROWS / 2 ? 2 : 1;
-    const int64_t at = (int64_t)h * __ldcg(&a.w.head->wide_cost) + g.cost0 + (int64_t)chunk * nt * w0;
+    const int64_t at = (int64_t)h * total + g.cost0 + (int64_t)chunk * nt * w0;
     end = (int)min((int64_t)nt, (stop - at + weight - 1) / weight);
     return end > tile;
   }
   __device__ __forceinline__ bool begin(const AttendArgs& a) {
-    const int4 st = __ldcg(reinterpret_cast<const int4*>(a.w.wide_start + blockIdx.x));
-    h = st.x; gi = st.y; chunk = st.z; tile = st.w;
-    if (h < 0) return false;
-    const int64_t each = __ldcg(&a.w.head->wide_each);
-    stop = min((int64_t)a.g.n_kv_heads * __ldcg(&a.w.head->wide_cost), (blockIdx.x + 1) * each);
-    g = load_group(a.w.groups + gi);
+    const AttendStart st = load_start(a.w.wide_start + blockIdx.x);
+    if (!plan_fits(a) || st.h < 0) return false;
+    h = st.h; gi = st.item; chunk = st.chunk; tile = st.tile;
+    g = st.group;
+    items = st.items; total = st.total; chunks = st.chunks;
+    stop = min((int64_t)a.g.n_kv_heads * total, (blockIdx.x + 1) * (int64_t)st.each);
     return set(a) || next(a);
   }
   __device__ __forceinline__ bool next(const AttendArgs& a) {
-    const int n = __ldcg(&a.w.head->n_groups);
     tile = 0;
     ++chunk;
     while (g.pfx == 0 || chunk * wide_tokens(a.group_heads) >= g.ntok) {
       chunk = 0;
-      if (++gi >= n) {
+      if (++gi >= items) {
         gi = 0;
         if (++h >= a.g.n_kv_heads) return false;
       }
@@ -77,11 +79,30 @@ struct Walk {
   __device__ __forceinline__ int keys(int t) const { return min(WIDE_KEYS, g.pfx - t * WIDE_KEYS); }
 };
 
-__device__ __forceinline__ float max_nan(float a, float b) {
+__device__ __forceinline__ float max3(float a, float b, float c) {        // NaN where one is
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
+__device__ __forceinline__ float row_max(const uint32_t (&x)[4][32]) {
+  float m[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    m[k] = __uint_as_float(x[k][0]);
+#pragma unroll
+    for (int e = 1; e < 31; e += 2) m[k] = max3(m[k], __uint_as_float(x[k][e]), __uint_as_float(x[k][e + 1]));
+    m[k] = max3(m[k], __uint_as_float(x[k][31]), m[k]);
+  }
+  return max3(max3(m[0], m[1], m[2]), m[3], m[3]);
+}
+// Which column pairs of 32 take the polynomial: see pair_is_poly of the scorer for what it is.
+constexpr int POLY_OF_32 = 8;
+__device__ __forceinline__ constexpr bool poly_pair(int i) { return ((i & 31) * POLY_OF_32) % 32 + POLY_OF_32 >= 32; }
+
+template <int N>
+__device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
 
 template <bool FP8>
 __global__ void __launch_bounds__(WideSmem<FP8>::THREADS, 1)
@@ -120,144 +141,18 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   const uint32_t tmem = *reinterpret_cast<const uint32_t*>(sm + S::MISC);
   pdl_wait_predecessor();
   pdl_release_successor();                 // it finds room when this grid's blocks leave
-  Walk w;
-  const bool any = plan_fits(a) && w.begin(a);
   const int G = a.group_heads, T = wide_tokens(G);
 
-  if (any && warp == 0) {
-    // =============================== copies =====================================
-    const int shift = a.g.page_shift, per = WIDE_KEYS >> shift, page = 1 << shift;
-    int run = 0, n = 0;                    // chunks whose queries are on their way; tiles of all chunks
-    bool ok = true, more = true;
-    while (ok && more) {
-      if (run > 0 && !mbar_wait(bar(S::QE), (run - 1) & 1, s_abort, 211, true)) { ok = false; break; }
-      ++run;
-      if (lane == 0) {
-        mbar_expect_tx(bar(S::QF), (uint32_t)(2 * 128 * G * T));
-        tma_load_3d(base, &tm_q, bar(S::QF), 0, w.h * G, w.g.tok0 + w.chunk * T);
-        tma_load_3d(base + S::Q_HALF, &tm_q, bar(S::QF), 64, w.h * G, w.g.tok0 + w.chunk * T);
-      }
-      __syncwarp();
-      const int32_t* row = a.g.table + (int64_t)w.g.slot * a.g.max_pages;
-      const int last = w.g.pfx >> shift;   // pages of the prefix
-      int first = w.tile * per;            // page numbers of 32 pages a lane each, and of the 32 after them
-      int ids = first + lane < last ? __ldcg(row + first + lane) : 0;
-      int ids2 = first + 32 + lane < last ? __ldcg(row + first + 32 + lane) : 0;
-      for (int t = w.tile; t < w.end; ++t, ++n) {
-        if (t * per >= first + 32) {       // (a tile has 8 pages at most, and 32 is a multiple of what it has)
-          first += 32;
-          ids = ids2;
-          ids2 = first + 32 + lane < last ? __ldcg(row + first + 32 + lane) : 0;
-        }
-        const int ks = n % K_RING, vs = n % S::V_RING, np = w.keys(t) >> shift;
-        // E4M3 tiles land in a ring of their own, from which they are widened into K's
-        const uint32_t kbar = FP8 ? bar(S::CF + (n & 1)) : bar(S::KF + ks), kfree = FP8 ? bar(S::CE + (n & 1)) : bar(S::KE + ks);
-        const uint32_t kd = base + (FP8 ? S::CODES + (n & 1) * TILE_HALF : S::K + ks * TILE_BYTES);
-        const uint32_t kpar = ((FP8 ? n >> 1 : n / K_RING) & 1) ^ 1;
-        if (!mbar_wait(kfree, kpar, s_abort, 212, true)) { ok = false; break; }
-        if (lane == 0) mbar_expect_tx(kbar, (uint32_t)(np * page * a.g.k_row));
-        __syncwarp();
-        for (int x = 0; x < np; ++x) {
-          const int id = __shfl_sync(0xffffffffu, ids, t * per + x - first);
-          const int r = (id * a.g.n_kv_heads + w.h) << shift;
-          if (lane == 0) {
-            tma_load_2d(kd + x * page * 128, &tm_k, kbar, 0, r);
-            if (!FP8) tma_load_2d(kd + TILE_HALF + x * page * 128, &tm_k, kbar, 64, r);
-          }
-        }
-        if (!mbar_wait(bar(S::VE + vs), ((n / S::V_RING) & 1) ^ 1, s_abort, 213, true)) {
-          ok = false;
-          ++n;                             // K of this tile is in flight
-          break;
-        }
-        if (lane == 0) mbar_expect_tx(bar(S::VF + vs), (uint32_t)(np * page * 256));
-        __syncwarp();
-        for (int x = 0; x < np; ++x) {
-          const int id = __shfl_sync(0xffffffffu, ids, t * per + x - first);
-          const int r = (id * a.g.n_kv_heads + w.h) << shift;
-          if (lane == 0) {
-            const uint32_t vd = base + S::V + vs * TILE_BYTES + x * page * 128;
-            tma_load_2d(vd, &tm_v, bar(S::VF + vs), 0, r);
-            tma_load_2d(vd + TILE_HALF, &tm_v, bar(S::VF + vs), 64, r);
-          }
-        }
-      }
-      if (ok) more = w.next(a);
-    }
-    if (!ok || *s_abort) {                 // copies in flight land before the block ends
-      for (int i = max(0, n - 3); i < n; ++i) {
-        if (FP8) { if (i >= n - 2) mbar_wait(bar(S::CF + (i & 1)), (i >> 1) & 1, s_abort, 214, false); }
-        else if (i >= n - K_RING) mbar_wait(bar(S::KF + i % K_RING), (i / K_RING) & 1, s_abort, 214, false);
-        if (i >= n - S::V_RING) mbar_wait(bar(S::VF + i % S::V_RING), (i / S::V_RING) & 1, s_abort, 215, false);
-      }
-      mbar_wait(bar(S::QF), (run - 1) & 1, s_abort, 216, false);
-    }
-  } else if (any && warp == 1) {
-    // =============================== products ===================================
-    int n = 0, pv[2] = {0, 0};             // tiles before this run; products P V of each stream so far
-    bool ok = true, more = true;
-    for (int run = 0; ok && more; ++run) {
-      const bool full = __shfl_sync(0xffffffffu, (int)w.full(), 0);
-      const int tile = __shfl_sync(0xffffffffu, w.tile, 0), nt = __shfl_sync(0xffffffffu, w.end, 0) - tile;
-      const int pfx = __shfl_sync(0xffffffffu, w.g.pfx, 0);
-      const int items = full ? 2 * nt : nt;
-      auto keys = [&](int j) { return min(WIDE_KEYS, pfx - (tile + j) * WIDE_KEYS); };
-      auto scores = [&](int i) {           // S of item i
-        const int j = full ? i >> 1 : i, s = i & 1, ks = (n + j) % K_RING;
-        if (!full || s == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::KF + ks), ((n + j) / K_RING) & 1, s_abort, 221, true));
-        if (!ok) return;
-        tc_fence_after();
-        const uint64_t qd = smem_desc(base + (full ? s : 0) * 128 * 128), kd = smem_desc(base + S::K + ks * TILE_BYTES);
-        const uint32_t id = instr_desc(128, keys(j));
-        if (elect_one()) {
-#pragma unroll
-          for (int x = 0; x < 8; ++x)
-            tc_mma(tmem + s * 128, qd + (x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2, kd + (x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2, id, x > 0);
-          tc_commit(bar(S::SF + s));
-          if (!full || s == 1) tc_commit(bar(S::KE + ks));
-          if (i + 1 == items) tc_commit(bar(S::QE));
-        }
-        __syncwarp();
-      };
-      ok = __all_sync(0xffffffffu, mbar_wait(bar(S::QF), run & 1, s_abort, 222, true));
-      if (ok) scores(0);
-      if (ok && items > 1) scores(1);
-      for (int i = 0; ok && i < items; ++i) {
-        const int j = full ? i >> 1 : i, s = i & 1, vs = (n + j) % S::V_RING;
-        ok = __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv[s] & 1, s_abort, 223, true));
-        if (ok && (!full || s == 0)) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
-        if (!ok) break;
-        tc_fence_after();
-        const uint64_t vd = smem_desc_mn(base + S::V + vs * TILE_BYTES, TILE_HALF);
-        const int steps = keys(j) >> 4;
-        const bool fresh = i < 2;          // the stream's first product of the run
-        if (elect_one()) {
-          for (int x = 0; x < steps; ++x)
-            tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + x * 8, vd + x * (2048 >> 4), instr_desc(128, 128) | B_MN_MAJOR, !fresh || x > 0);
-          tc_commit(bar(S::OD + s));
-          if (!full || s == 1) tc_commit(bar(S::VE + vs));
-        }
-        __syncwarp();
-        ++pv[s];
-        if (i + 2 < items) scores(i + 2);
-      }
-      n += nt;
-      if (ok) more = w.next(a);
-    }
-    if (!ok) {                             // nothing writes tensor memory when it is freed
-      if (elect_one()) {
-        tc_commit(bar(S::DRAIN));
-        mbar_wait(bar(S::DRAIN), 0, s_abort, 225, false);
-      }
-      __syncwarp();
-    }
-  } else if (any && warp >= 4 && warp < 12) {
+  if (warp >= 4 && warp < 12) {
+    take_registers<S::REGS_ROWS>();
+    Walk w;
+    const bool any = w.begin(a);
     // =============================== weights ====================================
     const int s = (warp - 4) >> 2, row = (threadIdx.x & 127);      // stream; row of its 128 = lane of tensor memory
     const uint32_t st = tmem + s * 128 + ((uint32_t)((warp & 3) * 32) << 16), ot = st + 256;
     int it = 0;                                                     // items of the stream so far
     bool ok = true, more = true;
-    while (ok && more) {
+    while (any && ok && more) {
       const bool full = w.full();
       const int r = full ? s * 128 + row : row;                     // row of the chunk
       const bool warp_has = (r & ~31) < w.rows;                     // of this warp's rows some exist
@@ -270,20 +165,19 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (!__all_sync(0xffffffffu, mbar_wait(bar(S::SF + s), it & 1, s_abort, 231, true))) { ok = false; break; }
         tc_fence_after();
         if (warp_has) {
-          uint32_t x[2][16];
-          // the row's largest logit; NaN stays NaN
-          float mx = -INFINITY;
-          tc_ld_lane(st, x[0]);
+          uint32_t x[4][32];
 #pragma unroll
-          for (int k = 0; k < WIDE_KEYS / 16; ++k) {
-            if (16 * k < nk) {
-              tc_ld_wait(x[k & 1]);
-              if (16 * (k + 1) < nk) tc_ld_lane(st + 16 * (k + 1), x[(k + 1) & 1]);
+          for (int k = 0; k < 4; ++k) tc_ld_lane32(st + 32 * k, x[k]);
+          tc_wait_loads();
 #pragma unroll
-              for (int e = 0; e < 16; ++e) mx = max_nan(mx, __uint_as_float(x[k & 1][e]));
-            }
+          for (int k = 0; k < 4; ++k) tc_landed(x[k]);
+          if (nk < WIDE_KEYS) {
+#pragma unroll
+            for (int k = 0; k < WIDE_KEYS; ++k)
+              if (k >= nk) x[k >> 5][k & 31] = 0xff800000u;         // -inf
           }
-          mx *= c;
+          // the row's largest logit; NaN stays NaN
+          float mx = row_max(x) * c;
           if (mx == INFINITY) mx = __int_as_float(0x7fffffff);      // infinite logits: the row is NaN, as in inf - inf
           const bool first = t == t0;
           if (first) {
@@ -311,24 +205,23 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           }
           const float ref = m == -INFINITY ? 0.0f : m;
           const f32x2 c2 = pk(c, c), m2 = pk(-ref, -ref);
-          tc_ld_lane(st, x[0]);
+          f32x2 l3 = pk(0.0f, 0.0f);
 #pragma unroll
-          for (int k = 0; k < WIDE_KEYS / 16; ++k) {
-            if (16 * k < nk) {
-              tc_ld_wait(x[k & 1]);
-              if (16 * (k + 1) < nk) tc_ld_lane(st + 16 * (k + 1), x[(k + 1) & 1]);
-              uint32_t p[8];
+          for (int k = 0; k < 2; ++k) {
+            uint32_t p[32];                                         // over columns that have been read
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const f32x2 y = ex2_pair_mufu(fma2(pku(x[k & 1][2 * e], x[k & 1][2 * e + 1]), c2, m2));
-                l2 = add2(l2, y);
-                float lo, hi;
-                upk(y, lo, hi);
-                p[e] = pack2(lo, hi);                               // rounded for the tensor core; l keeps them unrounded
-              }
-              tc_st_lane8(st + 8 * k, p);                           // over columns that have been read
+            for (int e = 0; e < 32; ++e) {
+              const int col = 64 * k + 2 * e;
+              const f32x2 z = fma2(pku(x[col >> 5][col & 31], x[col >> 5][(col & 31) + 1]), c2, m2);
+              const f32x2 y = poly_pair(e) ? ex2_pair_poly<false>(z) : ex2_pair_mufu(z);
+              if (e & 1) l3 = add2(l3, y); else l2 = add2(l2, y);
+              float lo, hi;
+              upk(y, lo, hi);
+              p[e] = pack2(lo, hi);                                 // rounded for the tensor core; l keeps them unrounded
             }
+            tc_st_lane32(st + 32 * k, p);
           }
+          l2 = add2(l2, l3);
           tc_st_wait();
         }
         tc_fence_before();
@@ -336,7 +229,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       }
       if (!ok) break;
       // the part: this stream's rows of the run
-      const int64_t slot = (int64_t)w.h * __ldcg(&a.w.head->wide_chunks) + w.g.chunk0 + w.chunk + blockIdx.x;
+      const int64_t slot = (int64_t)w.h * w.chunks + w.g.chunk0 + w.chunk + blockIdx.x;
       const int64_t at = slot * WIDE_ROWS + s * 128 + row;
       if (t0 < w.end) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar(S::OD + s), (it - 1) & 1, s_abort, 233, true))) { ok = false; break; }
@@ -362,34 +255,166 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       if (r < w.rows) a.w.wide_ml[at] = make_float2(t0 < w.end ? m : -INFINITY, hsum(l2));
       more = w.next(a);
     }
-  } else if (FP8 && any && warp >= 12) {
-    // =============================== widening ===================================
-    const int key = threadIdx.x & 127;
-    int n = 0;
-    bool ok = true, more = true;
-    while (ok && more) {
-      for (int t = w.tile; ok && t < w.end; ++t, ++n) {
-        const int cs = n & 1, ks = n % K_RING;
-        ok = mbar_wait(bar(S::CF + cs), (n >> 1) & 1, s_abort, 241, true) && mbar_wait(bar(S::KE + ks), ((n / K_RING) & 1) ^ 1, s_abort, 242, true);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const uint8_t* from = sm + S::CODES + cs * TILE_HALF + key * 128;
-        uint8_t* to = sm + S::K + ks * TILE_BYTES + key * 128;
-#pragma unroll
-        for (int x = 0; x < 8; ++x) {      // 16 codes: two 16-byte pieces of the key's bf16 row
-          const uint4 v = *reinterpret_cast<const uint4*>(from + ((x ^ (key & 7)) << 4));
-          uint8_t* half = to + (x >> 2) * TILE_HALF;
-          const int pc = (x & 3) * 2;
-          *reinterpret_cast<uint4*>(half + ((pc ^ (key & 7)) << 4)) =
-              make_uint4(e4m3_pair(v.x), e4m3_pair(v.x >> 16), e4m3_pair(v.y), e4m3_pair(v.y >> 16));
-          *reinterpret_cast<uint4*>(half + (((pc + 1) ^ (key & 7)) << 4)) =
-              make_uint4(e4m3_pair(v.z), e4m3_pair(v.z >> 16), e4m3_pair(v.w), e4m3_pair(v.w >> 16));
+  } else {
+    give_registers<S::REGS_FEW>();
+    Walk w;
+    const bool any = w.begin(a);
+    if (any && warp == 0) {
+      // =============================== copies =====================================
+      const int shift = a.g.page_shift, per = WIDE_KEYS >> shift, page = 1 << shift;
+      int run = 0, n = 0;                    // chunks whose queries are on their way; tiles of all chunks
+      bool ok = true, more = true;
+      while (ok && more) {
+        if (run > 0 && !mbar_wait(bar(S::QE), (run - 1) & 1, s_abort, 211, true)) { ok = false; break; }
+        ++run;
+        if (lane == 0) {
+          mbar_expect_tx(bar(S::QF), (uint32_t)(2 * 128 * G * T));
+          tma_load_3d(base, &tm_q, bar(S::QF), 0, w.h * G, w.g.tok0 + w.chunk * T);
+          tma_load_3d(base + S::Q_HALF, &tm_q, bar(S::QF), 64, w.h * G, w.g.tok0 + w.chunk * T);
         }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(bar(S::KF + ks));
-        mbar_arrive(bar(S::CE + cs));
+        __syncwarp();
+        const int32_t* row = a.g.table + (int64_t)w.g.slot * a.g.max_pages;
+        const int last = w.g.pfx >> shift;   // pages of the prefix
+        int first = w.tile * per;            // page numbers of 32 pages a lane each, and of the 32 after them
+        int ids = first + lane < last ? __ldcg(row + first + lane) : 0;
+        int ids2 = first + 32 + lane < last ? __ldcg(row + first + 32 + lane) : 0;
+        for (int t = w.tile; t < w.end; ++t, ++n) {
+          if (t * per >= first + 32) {       // (a tile has 8 pages at most, and 32 is a multiple of what it has)
+            first += 32;
+            ids = ids2;
+            ids2 = first + 32 + lane < last ? __ldcg(row + first + 32 + lane) : 0;
+          }
+          const int ks = n % K_RING, vs = n % S::V_RING, np = w.keys(t) >> shift;
+          // E4M3 tiles land in a ring of their own, from which they are widened into K's
+          const uint32_t kbar = FP8 ? bar(S::CF + (n & 1)) : bar(S::KF + ks), kfree = FP8 ? bar(S::CE + (n & 1)) : bar(S::KE + ks);
+          const uint32_t kd = base + (FP8 ? S::CODES + (n & 1) * TILE_HALF : S::K + ks * TILE_BYTES);
+          const uint32_t kpar = ((FP8 ? n >> 1 : n / K_RING) & 1) ^ 1;
+          if (!mbar_wait(kfree, kpar, s_abort, 212, true)) { ok = false; break; }
+          if (lane == 0) mbar_expect_tx(kbar, (uint32_t)(np * page * a.g.k_row));
+          __syncwarp();
+          for (int x = 0; x < np; ++x) {
+            const int id = __shfl_sync(0xffffffffu, ids, t * per + x - first);
+            const int r = (id * a.g.n_kv_heads + w.h) << shift;
+            if (lane == 0) {
+              tma_load_2d(kd + x * page * 128, &tm_k, kbar, 0, r);
+              if (!FP8) tma_load_2d(kd + TILE_HALF + x * page * 128, &tm_k, kbar, 64, r);
+            }
+          }
+          if (!mbar_wait(bar(S::VE + vs), ((n / S::V_RING) & 1) ^ 1, s_abort, 213, true)) {
+            ok = false;
+            ++n;                             // K of this tile is in flight
+            break;
+          }
+          if (lane == 0) mbar_expect_tx(bar(S::VF + vs), (uint32_t)(np * page * 256));
+          __syncwarp();
+          for (int x = 0; x < np; ++x) {
+            const int id = __shfl_sync(0xffffffffu, ids, t * per + x - first);
+            const int r = (id * a.g.n_kv_heads + w.h) << shift;
+            if (lane == 0) {
+              const uint32_t vd = base + S::V + vs * TILE_BYTES + x * page * 128;
+              tma_load_2d(vd, &tm_v, bar(S::VF + vs), 0, r);
+              tma_load_2d(vd + TILE_HALF, &tm_v, bar(S::VF + vs), 64, r);
+            }
+          }
+        }
+        if (ok) more = w.next(a);
       }
-      if (ok) more = w.next(a);
+      if (!ok || *s_abort) {                 // copies in flight land before the block ends
+        for (int i = max(0, n - 3); i < n; ++i) {
+          if (FP8) { if (i >= n - 2) mbar_wait(bar(S::CF + (i & 1)), (i >> 1) & 1, s_abort, 214, false); }
+          else if (i >= n - K_RING) mbar_wait(bar(S::KF + i % K_RING), (i / K_RING) & 1, s_abort, 214, false);
+          if (i >= n - S::V_RING) mbar_wait(bar(S::VF + i % S::V_RING), (i / S::V_RING) & 1, s_abort, 215, false);
+        }
+        mbar_wait(bar(S::QF), (run - 1) & 1, s_abort, 216, false);
+      }
+    } else if (any && warp == 1) {
+      // =============================== products ===================================
+      int n = 0, pv[2] = {0, 0};             // tiles before this run; products P V of each stream so far
+      bool ok = true, more = true;
+      for (int run = 0; ok && more; ++run) {
+        const bool full = __shfl_sync(0xffffffffu, (int)w.full(), 0);
+        const int tile = __shfl_sync(0xffffffffu, w.tile, 0), nt = __shfl_sync(0xffffffffu, w.end, 0) - tile;
+        const int pfx = __shfl_sync(0xffffffffu, w.g.pfx, 0);
+        const int items = full ? 2 * nt : nt;
+        auto keys = [&](int j) { return min(WIDE_KEYS, pfx - (tile + j) * WIDE_KEYS); };
+        auto scores = [&](int i) {           // S of item i
+          const int j = full ? i >> 1 : i, s = i & 1, ks = (n + j) % K_RING;
+          if (!full || s == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::KF + ks), ((n + j) / K_RING) & 1, s_abort, 221, true));
+          if (!ok) return;
+          tc_fence_after();
+          const uint64_t qd = smem_desc(base + (full ? s : 0) * 128 * 128), kd = smem_desc(base + S::K + ks * TILE_BYTES);
+          const uint32_t id = instr_desc(128, keys(j));
+          if (elect_one()) {
+  #pragma unroll
+            for (int x = 0; x < 8; ++x)
+              tc_mma(tmem + s * 128, qd + (x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2, kd + (x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2, id, x > 0);
+            tc_commit(bar(S::SF + s));
+            if (!full || s == 1) tc_commit(bar(S::KE + ks));
+            if (i + 1 == items) tc_commit(bar(S::QE));
+          }
+          __syncwarp();
+        };
+        ok = __all_sync(0xffffffffu, mbar_wait(bar(S::QF), run & 1, s_abort, 222, true));
+        if (ok) scores(0);
+        if (ok && items > 1) scores(1);
+        for (int i = 0; ok && i < items; ++i) {
+          const int j = full ? i >> 1 : i, s = i & 1, vs = (n + j) % S::V_RING;
+          ok = __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv[s] & 1, s_abort, 223, true));
+          if (ok && (!full || s == 0)) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t vd = smem_desc_mn(base + S::V + vs * TILE_BYTES, TILE_HALF);
+          const int steps = keys(j) >> 4;
+          const bool fresh = i < 2;          // the stream's first product of the run
+          if (elect_one()) {
+            for (int x = 0; x < steps; ++x)
+              tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + x * 8, vd + x * (2048 >> 4), instr_desc(128, 128) | B_MN_MAJOR, !fresh || x > 0);
+            tc_commit(bar(S::OD + s));
+            if (!full || s == 1) tc_commit(bar(S::VE + vs));
+          }
+          __syncwarp();
+          ++pv[s];
+          if (i + 2 < items) scores(i + 2);
+        }
+        n += nt;
+        if (ok) more = w.next(a);
+      }
+      if (!ok) {                             // nothing writes tensor memory when it is freed
+        if (elect_one()) {
+          tc_commit(bar(S::DRAIN));
+          mbar_wait(bar(S::DRAIN), 0, s_abort, 225, false);
+        }
+        __syncwarp();
+      }
+    } else if (FP8 && any && warp >= 12) {
+      // =============================== widening ===================================
+      const int key = threadIdx.x & 127;
+      int n = 0;
+      bool ok = true, more = true;
+      while (ok && more) {
+        for (int t = w.tile; ok && t < w.end; ++t, ++n) {
+          const int cs = n & 1, ks = n % K_RING;
+          ok = mbar_wait(bar(S::CF + cs), (n >> 1) & 1, s_abort, 241, true) && mbar_wait(bar(S::KE + ks), ((n / K_RING) & 1) ^ 1, s_abort, 242, true);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          const uint8_t* from = sm + S::CODES + cs * TILE_HALF + key * 128;
+          uint8_t* to = sm + S::K + ks * TILE_BYTES + key * 128;
+  #pragma unroll
+          for (int x = 0; x < 8; ++x) {      // 16 codes: two 16-byte pieces of the key's bf16 row
+            const uint4 v = *reinterpret_cast<const uint4*>(from + ((x ^ (key & 7)) << 4));
+            uint8_t* half = to + (x >> 2) * TILE_HALF;
+            const int pc = (x & 3) * 2;
+            *reinterpret_cast<uint4*>(half + ((pc ^ (key & 7)) << 4)) =
+                make_uint4(e4m3_pair(v.x), e4m3_pair(v.x >> 16), e4m3_pair(v.y), e4m3_pair(v.y >> 16));
+            *reinterpret_cast<uint4*>(half + (((pc + 1) ^ (key & 7)) << 4)) =
+                make_uint4(e4m3_pair(v.z), e4m3_pair(v.z >> 16), e4m3_pair(v.w), e4m3_pair(v.w >> 16));
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_arrive(bar(S::KF + ks));
+          mbar_arrive(bar(S::CE + cs));
+        }
+        if (ok) more = w.next(a);
+      }
     }
   }
   tc_fence_before();
