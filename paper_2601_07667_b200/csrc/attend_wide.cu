@@ -120,7 +120,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     for (int i = 0; i < S::V_RING; ++i) { mbar_init(bar(S::VF + i), 1); mbar_init(bar(S::VE + i), 1); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(S::SF + i), 1);
-      mbar_init(bar(S::PF + i), 128);
+      mbar_init(bar(S::PF + i), 4);
       mbar_init(bar(S::OD + i), 1);
       mbar_init(bar(S::CF + i), 1);
       mbar_init(bar(S::CE + i), 128);
@@ -225,7 +225,8 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           tc_st_wait();
         }
         tc_fence_before();
-        mbar_arrive(bar(S::PF + s));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(S::PF + s));
       }
       if (!ok) break;
       // the part: this stream's rows of the run
@@ -329,25 +330,29 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       }
     } else if (any && warp == 1) {
       // =============================== products ===================================
-      int n = 0, pv[2] = {0, 0};             // tiles before this run; products P V of each stream so far
+      // (What the products' operands follow from is shuffled, so that the compiler knows it to be the same in all lanes and
+      // keeps descriptors in uniform registers: moved there one by one they cost 100 clk a product instead of 64.)
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      const uint32_t id_full = instr_desc(128, WIDE_KEYS), id_pv = instr_desc(128, 128) | B_MN_MAJOR;
+      int n = 0;                           // tiles before this run
+      uint32_t pv[2] = {0, 0};             // parity of each stream's next product P V
       bool ok = true, more = true;
       for (int run = 0; ok && more; ++run) {
         const bool full = __shfl_sync(0xffffffffu, (int)w.full(), 0);
         const int tile = __shfl_sync(0xffffffffu, w.tile, 0), nt = __shfl_sync(0xffffffffu, w.end, 0) - tile;
-        const int pfx = __shfl_sync(0xffffffffu, w.g.pfx, 0);
+        const int pfx = __shfl_sync(0xffffffffu, w.g.pfx, 0) - tile * WIDE_KEYS;      // keys from the first tile on
         const int items = full ? 2 * nt : nt;
-        auto keys = [&](int j) { return min(WIDE_KEYS, pfx - (tile + j) * WIDE_KEYS); };
-        auto scores = [&](int i) {           // S of item i
-          const int j = full ? i >> 1 : i, s = i & 1, ks = (n + j) % K_RING;
+        auto scores = [&](int i) {         // S of item i
+          const int j = full ? i >> 1 : i, s = i & 1, ks = (n + j) % K_RING, left = pfx - j * WIDE_KEYS;
           if (!full || s == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::KF + ks), ((n + j) / K_RING) & 1, s_abort, 221, true));
           if (!ok) return;
           tc_fence_after();
           const uint64_t qd = smem_desc(base + (full ? s : 0) * 128 * 128), kd = smem_desc(base + S::K + ks * TILE_BYTES);
-          const uint32_t id = instr_desc(128, keys(j));
+          const uint32_t id = left >= WIDE_KEYS ? id_full : instr_desc(128, left);
           if (elect_one()) {
-  #pragma unroll
+#pragma unroll
             for (int x = 0; x < 8; ++x)
-              tc_mma(tmem + s * 128, qd + (x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2, kd + (x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2, id, x > 0);
+              tc_mma(tm + s * 128, qd + ((x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2), kd + ((x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2), id, x > 0);
             tc_commit(bar(S::SF + s));
             if (!full || s == 1) tc_commit(bar(S::KE + ks));
             if (i + 1 == items) tc_commit(bar(S::QE));
@@ -358,28 +363,33 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (ok) scores(0);
         if (ok && items > 1) scores(1);
         for (int i = 0; ok && i < items; ++i) {
-          const int j = full ? i >> 1 : i, s = i & 1, vs = (n + j) % S::V_RING;
-          ok = __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv[s] & 1, s_abort, 223, true));
-          if (ok && (!full || s == 0)) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+          const int j = full ? i >> 1 : i, s = i & 1, vs = (n + j) % S::V_RING, left = pfx - j * WIDE_KEYS;
+          if (!full || s == 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv[s], s_abort, 223, true));
           if (!ok) break;
           tc_fence_after();
           const uint64_t vd = smem_desc_mn(base + S::V + vs * TILE_BYTES, TILE_HALF);
-          const int steps = keys(j) >> 4;
-          const bool fresh = i < 2;          // the stream's first product of the run
+          const uint32_t fresh = i < 2;    // the stream's first product of the run
           if (elect_one()) {
-            for (int x = 0; x < steps; ++x)
-              tc_mma_ts(tmem + 256 + s * 128, tmem + s * 128 + x * 8, vd + x * (2048 >> 4), instr_desc(128, 128) | B_MN_MAJOR, !fresh || x > 0);
+            if (left >= WIDE_KEYS) {
+#pragma unroll
+              for (int x = 0; x < 8; ++x)
+                tc_mma_ts(tm + 256 + s * 128, tm + s * 128 + x * 8, vd + x * (2048 >> 4), id_pv, x > 0 ? 1u : fresh ^ 1u);
+            } else {
+              for (int x = 0; x < left >> 4; ++x)
+                tc_mma_ts(tm + 256 + s * 128, tm + s * 128 + x * 8, vd + x * (2048 >> 4), id_pv, x > 0 ? 1u : fresh ^ 1u);
+            }
             tc_commit(bar(S::OD + s));
             if (!full || s == 1) tc_commit(bar(S::VE + vs));
           }
           __syncwarp();
-          ++pv[s];
+          pv[s] ^= 1u;
           if (i + 2 < items) scores(i + 2);
         }
         n += nt;
         if (ok) more = w.next(a);
       }
-      if (!ok) {                             // nothing writes tensor memory when it is freed
+      if (!ok) {                           // nothing writes tensor memory when it is freed
         if (elect_one()) {
           tc_commit(bar(S::DRAIN));
           mbar_wait(bar(S::DRAIN), 0, s_abort, 225, false);
