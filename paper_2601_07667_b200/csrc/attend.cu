@@ -79,7 +79,7 @@ struct PlanArgs {
 __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   extern __shared__ int32_t sm[];
   __shared__ int part[PLAN_THREADS / 32];
-  __shared__ int n_groups_s;
+  __shared__ int n_groups_s, any_full;
   __shared__ unsigned long long most_s;
   pdl_wait_predecessor();
   const int tid = threadIdx.x, n = a.b.n_seqs, G = a.G;
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   int32_t* gpfx = first + n + 1;           // per group: shared tokens, first entry, wide cost before
   int32_t* gat = gpfx + n;
   int32_t* gcost = gat + n;                // [n + 1]
-  if (tid == 0) { a.w.head->made_for[0] = 0; most_s = 0; }
+  if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; }
   __syncthreads();
   for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tok_seq[t] = make_int2(-1, -1);
   for (int i = tid; i < n; i += PLAN_THREADS) {
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     if (ntok[i]) atomicAdd(&most_s, (unsigned long long)narrow_chunks_of(ntok[i], G) * (unsigned)(len[i] / NARROW_KEYS + 2));
   }
   __syncthreads();
-  if (most_s >= 1ull << 30) {
+  if (most_s * a.g.n_kv_heads >= 1ull << 30) {
     if (tid == 0) note_error(a.g.err, ASL_ERR_UNSUPPORTED, -1);
     return;
   }
@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       if (gpfx[i]) {
         c = wide_group_cost(tokens, gpfx[i], G);
         nc = (tokens + wide_tokens(G) - 1) / wide_tokens(G);
+        if (tokens * G > WIDE_ROWS / 2) any_full = 1;
       }
     }
     int csum, nsum;
@@ -210,16 +211,17 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   if (tid == 0) { first[n] = tiles; gcost[ng] = cost; }
   __syncthreads();
   const int H = a.g.n_kv_heads;
-  const int narrow_each = max(1, (int)(((int64_t)H * tiles + a.narrow_grid - 1) / a.narrow_grid));
-  const int wide_each = max(2, (int)(((int64_t)H * cost + a.wide_grid - 1) / a.wide_grid));
+  const int narrow_each = max(1, (H * tiles + a.narrow_grid - 1) / a.narrow_grid);
+  // (a stretch has to hold the beginning of a tile, whose cost is 2 in chunks of more than 128 rows)
+  const int wide_each = max(any_full ? 2 : 1, (H * cost + a.wide_grid - 1) / a.wide_grid);
   for (int k = tid; k < a.narrow_grid; k += PLAN_THREADS) {
     AttendStart s = {};
     s.h = -1;
     s.items = n; s.total = tiles; s.chunks = chunks; s.each = narrow_each;
     const int64_t u = (int64_t)k * narrow_each;
-    if (u < (int64_t)H * tiles) {
-      s.h = (int)(u / tiles);
-      const int r = (int)(u % tiles);
+    if (u < H * tiles) {
+      s.h = (int)u / tiles;
+      const int r = (int)u % tiles;
       int lo = 0, hi = n;                                       // last entry with first <= r that has tiles
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
@@ -238,9 +240,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     s.h = -1;
     s.items = ng; s.total = cost; s.chunks = wchunks; s.each = wide_each;
     const int64_t u = (int64_t)k * wide_each;
-    if (u < (int64_t)H * cost) {
-      s.h = (int)(u / cost);
-      const int r = (int)(u % cost);
+    if (u < H * cost) {
+      s.h = (int)u / cost;
+      const int r = (int)u % cost;
       int lo = 0, hi = ng;
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
@@ -260,20 +262,20 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   }
   __syncthreads();
   if (tid == 0) {
-    AttendHead* h = a.w.head;
-    h->n_seqs = n;
-    h->n_groups = ng;
-    h->narrow_tiles = tiles;
-    h->narrow_chunks = chunks;
-    h->narrow_each = narrow_each;
-    h->wide_cost = cost;
-    h->wide_chunks = wchunks;
-    h->wide_each = wide_each;
-    h->made_for[0] = ATTEND_MARK;
-    h->made_for[1] = n;
-    h->made_for[2] = a.b.n_tokens;
-    h->made_for[3] = a.n_q_heads;
-    h->made_for[4] = a.g.n_kv_heads;
+    AttendHead h;
+    h.mark = ATTEND_MARK;
+    h.n_seqs = n;
+    h.n_tokens = a.b.n_tokens;
+    h.n_q_heads = a.n_q_heads;
+    h.n_kv_heads = H;
+    h.n_groups = ng;
+    h.narrow_tiles = tiles;
+    h.narrow_chunks = chunks;
+    h.narrow_each = narrow_each;
+    h.wide_cost = cost;
+    h.wide_chunks = wchunks;
+    h.wide_each = wide_each;
+    *a.w.head = h;
   }
 }
 
@@ -289,28 +291,26 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
   const bool exists = row < a.n_tokens * a.n_q_heads;
   const int t = exists ? row / a.n_q_heads : 0, head = row - t * a.n_q_heads, G = a.group_heads, h = head / G, g = head - h * G;
   const int2 who = __ldcg(a.w.tok_seq + t);
-  const AttendHead* hd = a.w.head;
-  const int n_tiles = __ldcg(&hd->narrow_tiles), n_chunks = __ldcg(&hd->narrow_chunks), n_each = __ldcg(&hd->narrow_each);
-  const int w_cost = __ldcg(&hd->wide_cost), w_chunks = __ldcg(&hd->wide_chunks), w_each = __ldcg(&hd->wide_each);
-  if (!plan_fits(a) || !exists || who.x < 0) return;              // (the same for all warps of a row)
+  const AttendHead hd = load_head(a.w.head);
+  if (!plan_fits(a, hd) || !exists || who.x < 0) return;              // (the same for all warps of a row)
   const AttendSeq s = load_seq(a.w.seqs + who.x);
   const AttendGroup gr = load_group(a.w.groups + who.y);
   const int nt = narrow_tiles_of(s), lr = (t - s.tok0) * G + g, chunk = lr / NARROW_ROWS;
-  const int64_t ta = (int64_t)h * n_tiles + s.tile0 + (int64_t)chunk * nt;
-  const int c0 = (int)(ta / n_each), c1 = (int)((ta + nt - 1) / n_each);
+  const int ta = h * hd.narrow_tiles + s.tile0 + chunk * nt;
+  const int c0 = ta / hd.narrow_each, c1 = (ta + nt - 1) / hd.narrow_each;
   if (s.pfx == 0 && c0 == c1) return;                             // written where it was computed
   // parts: narrow ones c0 .. c1, then those of the prefix (two halves each where a chunk's rows fill one)
-  const int64_t n_row = ((int64_t)h * n_chunks + s.chunk0 + chunk + c0) * NARROW_ROWS + lr % NARROW_ROWS;
+  const int64_t n_row = ((int64_t)h * hd.narrow_chunks + s.chunk0 + chunk + c0) * NARROW_ROWS + lr % NARROW_ROWS;
   const int n_parts = c1 - c0 + 1;
   int64_t w_row = 0;
   int total = n_parts, w_step = 0;
   if (s.pfx) {
     const int T = wide_tokens(G), ch = (t - gr.tok0) / T, wr = ((t - gr.tok0) - ch * T) * G + g;
     const int wt = (gr.pfx + WIDE_KEYS - 1) / WIDE_KEYS, w = wide_weight(gr, ch, G), w0 = T * G > WIDE_ROWS / 2 ? 2 : 1;
-    const int64_t a0 = (int64_t)h * w_cost + gr.cost0 + (int64_t)ch * wt * w0;
-    const int x0 = (int)(a0 / w_each), x1 = (int)((a0 + (int64_t)(wt - 1) * w) / w_each);
+    const int a0 = h * hd.wide_cost + gr.cost0 + ch * wt * w0;
+    const int x0 = a0 / hd.wide_each, x1 = (a0 + (wt - 1) * w) / hd.wide_each;
     const int halves = w == 1 ? 2 : 1;
-    w_row = ((int64_t)h * w_chunks + gr.chunk0 + ch + x0) * WIDE_ROWS + wr;
+    w_row = ((int64_t)h * hd.wide_chunks + gr.chunk0 + ch + x0) * WIDE_ROWS + wr;
     w_step = WIDE_ROWS / halves;
     total += (x1 - x0 + 1) * halves;
   }

@@ -14,11 +14,10 @@ constexpr int NARROW_ROWS = 16, NARROW_KEYS = 64;
 constexpr int WIDE_ROWS = 256, WIDE_KEYS = 128;
 constexpr int ATTEND_MAX_SEQS = 4096;
 
-struct AttendHead {        // one per plan, on the device
-  int32_t n_seqs, n_groups;
-  int32_t narrow_tiles, narrow_chunks, narrow_each;   // per kv head; tiles per CTA
-  int32_t wide_cost, wide_chunks, wide_each;          // per kv head; cost per CTA (at least 2)
-  int32_t made_for[5];                                // sizes the layout follows from, and a mark: see plan_fits
+struct __align__(16) AttendHead {        // one per plan, on the device
+  int32_t mark, n_seqs, n_tokens, n_q_heads;          // what the layout follows from: see plan_fits
+  int32_t n_kv_heads, n_groups, narrow_tiles, narrow_chunks;   // tiles and chunks per kv head
+  int32_t narrow_each, wide_cost, wide_chunks, wide_each;      // tiles and cost per CTA; cost and chunks per kv head
 };
 constexpr int ATTEND_MARK = 0x41534c50;
 struct __align__(16) AttendSeq {
@@ -76,11 +75,21 @@ __device__
 inline int wide_tokens(int G) { return WIDE_ROWS / G; }
 
 #ifdef __CUDACC__
+// Every warp reads the head: by loads that L1 keeps (written two launches ago or more), since thousands of requests for one
+// line wait for one another in L2 (the joined rows of 32 sequences with 32 heads: 13 us, of which 8.7 were these loads).
+__device__ __forceinline__ AttendHead load_head(const AttendHead* h) {
+  AttendHead r;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    int4& q = reinterpret_cast<int4*>(&r)[i];
+    asm volatile("ld.global.ca.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(reinterpret_cast<const int4*>(h) + i) : "memory");
+  }
+  return r;
+}
 // A workspace that holds no plan, or one for other sizes, is refused before anything is read through it.
-__device__ __forceinline__ bool plan_fits(const AttendArgs& a) {
-  const int32_t* m = a.w.head->made_for;
-  const bool fits = __ldcg(m) == ATTEND_MARK && __ldcg(m + 1) == a.n_seqs && __ldcg(m + 2) == a.n_tokens &&
-                    __ldcg(m + 3) == a.n_q_heads && __ldcg(m + 4) == a.g.n_kv_heads;
+__device__ __forceinline__ bool plan_fits(const AttendArgs& a, const AttendHead& h) {
+  const bool fits = h.mark == ATTEND_MARK && h.n_seqs == a.n_seqs && h.n_tokens == a.n_tokens && h.n_q_heads == a.n_q_heads &&
+                    h.n_kv_heads == a.g.n_kv_heads;
   if (!fits && threadIdx.x == 0) note_error(a.g.err, ASL_ERR_WORKSPACE, -1);
   return fits;
 }

@@ -48,12 +48,13 @@ struct Walk {
     nch = narrow_chunks_of(s.ntok, a.group_heads);
   }
   __device__ __forceinline__ bool begin(const AttendArgs& a) {
+    const AttendHead hd = load_head(a.w.head);
     const AttendStart st = load_start(a.w.narrow_start + blockIdx.x);
-    if (!plan_fits(a) || st.h < 0) return false;
+    if (!plan_fits(a, hd) || st.h < 0) return false;
     h = st.h; i = st.item; chunk = st.chunk; tile = st.tile;
     s = st.seq;
     items = st.items; total = st.total; chunks = st.chunks; each = st.each;
-    left = (int)min((int64_t)each, (int64_t)a.g.n_kv_heads * total - (int64_t)blockIdx.x * each);
+    left = min(each, a.g.n_kv_heads * total - (int)blockIdx.x * each);
     sizes(a);
     return true;
   }
@@ -77,7 +78,7 @@ struct Walk {
   }
   // A chunk whose keys nobody else has part of: its rows are written at once.
   __device__ __forceinline__ bool sole() const {
-    const int64_t at = (int64_t)h * total + s.tile0 + (int64_t)chunk * nt;
+    const int at = h * total + s.tile0 + chunk * nt;
     return s.pfx == 0 && at / each == (at + nt - 1) / each;
   }
   __device__ __forceinline__ int64_t slot() const { return (int64_t)h * chunks + s.chunk0 + chunk + blockIdx.x; }

@@ -41,7 +41,7 @@ struct WideSmem {
 struct Walk {
   int h, gi, chunk, tile, end;
   int nt, weight, rows, items, total, chunks;
-  int64_t stop;                            // cost at which the stretch ends
+  int stop;                                // cost at which the stretch ends
   AttendGroup g;
   __device__ __forceinline__ bool set(const AttendArgs& a) {        // a chunk of group g: its tiles in the stretch
     const int T = wide_tokens(a.group_heads);
@@ -49,17 +49,18 @@ struct Walk {
     weight = wide_weight(g, chunk, a.group_heads);
     rows = min(T, g.ntok - chunk * T) * a.group_heads;
     const int w0 = T * a.group_heads > WIDE_ROWS / 2 ? 2 : 1;
-    const int64_t at = (int64_t)h * total + g.cost0 + (int64_t)chunk * nt * w0;
-    end = (int)min((int64_t)nt, (stop - at + weight - 1) / weight);
+    const int at = h * total + g.cost0 + chunk * nt * w0;
+    end = min(nt, (stop - at + weight - 1) / weight);
     return end > tile;
   }
   __device__ __forceinline__ bool begin(const AttendArgs& a) {
+    const AttendHead hd = load_head(a.w.head);
     const AttendStart st = load_start(a.w.wide_start + blockIdx.x);
-    if (!plan_fits(a) || st.h < 0) return false;
+    if (!plan_fits(a, hd) || st.h < 0) return false;
     h = st.h; gi = st.item; chunk = st.chunk; tile = st.tile;
     g = st.group;
     items = st.items; total = st.total; chunks = st.chunks;
-    stop = min((int64_t)a.g.n_kv_heads * total, (blockIdx.x + 1) * (int64_t)st.each);
+    stop = min(a.g.n_kv_heads * total, ((int)blockIdx.x + 1) * st.each);
     return set(a) || next(a);
   }
   __device__ __forceinline__ bool next(const AttendArgs& a) {
@@ -342,11 +343,18 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int tile = __shfl_sync(0xffffffffu, w.tile, 0), nt = __shfl_sync(0xffffffffu, w.end, 0) - tile;
         const int pfx = __shfl_sync(0xffffffffu, w.g.pfx, 0) - tile * WIDE_KEYS;      // keys from the first tile on
         const int items = full ? 2 * nt : nt;
+        auto keys_here = [&](int i) {      // the tile of item i's keys
+          const int j = full ? i >> 1 : i, ks = (n + j) % K_RING;
+          if (ok && i < items && (!full || !(i & 1)))
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::KF + ks), ((n + j) / K_RING) & 1, s_abort, 221, true));
+        };
+        auto values_here = [&](int i) {
+          const int j = full ? i >> 1 : i, vs = (n + j) % S::V_RING;
+          if (ok && i < items && (!full || !(i & 1)))
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+        };
         auto scores = [&](int i) {         // S of item i
           const int j = full ? i >> 1 : i, s = i & 1, ks = (n + j) % K_RING, left = pfx - j * WIDE_KEYS;
-          if (!full || s == 0) ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::KF + ks), ((n + j) / K_RING) & 1, s_abort, 221, true));
-          if (!ok) return;
-          tc_fence_after();
           const uint64_t qd = smem_desc(base + (full ? s : 0) * 128 * 128), kd = smem_desc(base + S::K + ks * TILE_BYTES);
           const uint32_t id = left >= WIDE_KEYS ? id_full : instr_desc(128, left);
           if (elect_one()) {
@@ -360,11 +368,16 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           __syncwarp();
         };
         ok = __all_sync(0xffffffffu, mbar_wait(bar(S::QF), run & 1, s_abort, 222, true));
+        keys_here(0);
+        tc_fence_after();
         if (ok) scores(0);
+        keys_here(1);
         if (ok && items > 1) scores(1);
         for (int i = 0; ok && i < items; ++i) {
           const int j = full ? i >> 1 : i, s = i & 1, vs = (n + j) % S::V_RING, left = pfx - j * WIDE_KEYS;
-          if (!full || s == 0) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+          // (tiles are waited for before the weights, while the tensor pipe still has products of the item before)
+          values_here(i);
+          keys_here(i + 2);
           ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv[s], s_abort, 223, true));
           if (!ok) break;
           tc_fence_after();
