@@ -176,48 +176,65 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     tiles += tsum;
     chunks += csum;
   }
+  // groups: their cost, from it what a CTA has of it and the stripes, then the chunks of stripes
+  int32_t* gtok = ntok;                    // a group's tokens (the entries' are not needed any more)
   int cost = 0, wchunks = 0;
+  __syncthreads();
   for (int i0 = 0; i0 < ng; i0 += PLAN_THREADS) {
     const int i = i0 + tid;
-    int c = 0, nc = 0, tokens = 0, at = 0, last = 0;
+    int c = 0, tokens = 0;
     if (i < ng) {
-      at = gat[i];
-      last = i + 1 < ng ? gat[i + 1] : n;
-      while (last > at + 1 && ntok[last - 1] == 0) --last;      // padding behind the group
-      tokens = __ldcg(a.b.cu_q + last - 1) + ntok[last - 1] - __ldcg(a.b.cu_q + at);
-      if (gpfx[i]) {
-        c = wide_group_cost(tokens, gpfx[i], G);
-        nc = (tokens + wide_tokens(G) - 1) / wide_tokens(G);
-        if (tokens * G > WIDE_ROWS / 2) any_full = 1;
-      }
+      const int at = gat[i];
+      int last = i + 1 < ng ? gat[i + 1] : n;
+      while (last > at + 1 && grp[last - 1] != i) --last;         // padding behind the group
+      tokens = a.w.seqs[last - 1].tok0 + a.w.seqs[last - 1].ntok - a.w.seqs[at].tok0;
+      const WideShape w(tokens, gpfx[i], G, 1);
+      c = w.tiles * w.sum;
+      if (gpfx[i] && tokens * G > WIDE_ROWS / 2) any_full = 1;
     }
-    int csum, nsum;
-    const int c0 = cost + scan_step(c, part, csum), n0 = wchunks + scan_step(nc, part, nsum);
+    int csum;
+    const int c0 = cost + scan_step(c, part, csum);
     if (i < ng) {
       gcost[i] = c0;
-      AttendGroup r;
-      r.tok0 = __ldcg(a.b.cu_q + at);
-      r.ntok = tokens;
-      r.slot = __ldcg(a.b.slots + at);
-      r.pfx = gpfx[i];
-      r.cost0 = c0;
-      r.chunk0 = n0;
-      r.pad0 = r.pad1 = 0;
-      a.w.groups[i] = r;
+      gtok[i] = tokens;                                           // (i <= every entry of groups still to come)
     }
     cost += csum;
+  }
+  __syncthreads();
+  const int H = a.g.n_kv_heads;
+  // (a stretch has to hold the beginning of a tile, whose cost is 2 in chunks of more than 128 rows)
+  const int wide_each = max(any_full ? 2 : 1, (H * cost + a.wide_grid - 1) / a.wide_grid);
+  const int stripe = (wide_each + 1) / 2;
+  for (int i0 = 0; i0 < ng; i0 += PLAN_THREADS) {
+    const int i = i0 + tid;
+    int nc = 0;
+    if (i < ng && gpfx[i]) {
+      const WideShape w(gtok[i], gpfx[i], G, stripe);
+      nc = w.chunks * w.stripes;
+    }
+    int nsum;
+    const int n0 = wchunks + scan_step(nc, part, nsum);
+    if (i < ng) {
+      AttendGroup r;
+      r.tok0 = a.w.seqs[gat[i]].tok0;
+      r.ntok = gtok[i];
+      r.slot = a.w.seqs[gat[i]].slot;
+      r.pfx = gpfx[i];
+      r.cost0 = gcost[i];
+      r.chunk0 = n0;
+      r.stripe = stripe;
+      r.pad0 = 0;
+      a.w.groups[i] = r;
+    }
     wchunks += nsum;
   }
   if (tid == 0) { first[n] = tiles; gcost[ng] = cost; }
   __syncthreads();
-  const int H = a.g.n_kv_heads;
   const int narrow_each = max(1, (H * tiles + a.narrow_grid - 1) / a.narrow_grid);
-  // (a stretch has to hold the beginning of a tile, whose cost is 2 in chunks of more than 128 rows)
-  const int wide_each = max(any_full ? 2 : 1, (H * cost + a.wide_grid - 1) / a.wide_grid);
   for (int k = tid; k < a.narrow_grid; k += PLAN_THREADS) {
     AttendStart s = {};
     s.h = -1;
-    s.items = n; s.total = tiles; s.chunks = chunks; s.each = narrow_each;
+    s.items = n; s.total = tiles; s.chunks = chunks; s.more = narrow_each;
     const int64_t u = (int64_t)k * narrow_each;
     if (u < H * tiles) {
       s.h = (int)u / tiles;
@@ -238,7 +255,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   for (int k = tid; k < a.wide_grid; k += PLAN_THREADS) {
     AttendStart s = {};
     s.h = -1;
-    s.items = ng; s.total = cost; s.chunks = wchunks; s.each = wide_each;
+    s.items = ng; s.total = cost; s.chunks = wchunks;
     const int64_t u = (int64_t)k * wide_each;
     if (u < H * cost) {
       s.h = (int)u / cost;
@@ -249,14 +266,15 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
         if (gcost[mid] <= r) lo = mid; else hi = mid;
       }
       s.item = lo;
-      const int nt = (gpfx[lo] + WIDE_KEYS - 1) / WIDE_KEYS, T = wide_tokens(G), w = T * G > WIDE_ROWS / 2 ? 2 : 1;
-      int x = r - gcost[lo];
       s.group = a.w.groups[lo];
-      const int whole = s.group.ntok / T;                       // full chunks first; the last one may count less
-      s.chunk = min(x / (nt * w), whole);
-      x -= s.chunk * nt * w;
-      const int wl = s.chunk < whole ? w : s.group.ntok % T * G > WIDE_ROWS / 2 ? 2 : 1;
-      s.tile = (x + wl - 1) / wl;                               // the first tile that begins in the stretch; may be the chunk's end
+      const WideShape w(s.group.ntok, s.group.pfx, G, stripe);
+      const int x = r - gcost[lo];
+      s.more = x / (w.stripe * w.sum);
+      const int y = x - s.more * w.stripe * w.sum, nt = w.tiles_of(s.more);
+      s.chunk = min(y / (nt * 2), w.whole);                       // full chunks first; the last one may cost less
+      if (s.chunk == w.chunks) s.chunk = w.chunks - 1;
+      const int z = y - s.chunk * nt * 2, wl = w.weight(s.chunk, G);
+      s.tile = s.more * w.stripe + (z + wl - 1) / wl;             // the first tile that begins in the stretch; may be the chunk's end
     }
     a.w.wide_start[k] = s;
   }
@@ -299,52 +317,70 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
   const int ta = h * hd.narrow_tiles + s.tile0 + chunk * nt;
   const int c0 = ta / hd.narrow_each, c1 = (ta + nt - 1) / hd.narrow_each;
   if (s.pfx == 0 && c0 == c1) return;                             // written where it was computed
-  // parts: narrow ones c0 .. c1, then those of the prefix (two halves each where a chunk's rows fill one)
+  // Parts: narrow ones c0 .. c1, then those of the prefix: two halves each where a chunk's rows fill one; where there are
+  // stripes, two CTAs each at most.
   const int64_t n_row = ((int64_t)h * hd.narrow_chunks + s.chunk0 + chunk + c0) * NARROW_ROWS + lr % NARROW_ROWS;
   const int n_parts = c1 - c0 + 1;
-  int64_t w_row = 0;
-  int total = n_parts, w_step = 0;
+  const WideShape ws(gr.ntok, s.pfx, G, gr.stripe);
+  int total = n_parts, halves = 1, ch = 0, wr = 0, weight = 2, x0 = 0;
+  const int h_cost = h * hd.wide_cost + gr.cost0;
   if (s.pfx) {
-    const int T = wide_tokens(G), ch = (t - gr.tok0) / T, wr = ((t - gr.tok0) - ch * T) * G + g;
-    const int wt = (gr.pfx + WIDE_KEYS - 1) / WIDE_KEYS, w = wide_weight(gr, ch, G), w0 = T * G > WIDE_ROWS / 2 ? 2 : 1;
-    const int a0 = h * hd.wide_cost + gr.cost0 + ch * wt * w0;
-    const int x0 = a0 / hd.wide_each, x1 = (a0 + (wt - 1) * w) / hd.wide_each;
-    const int halves = w == 1 ? 2 : 1;
-    w_row = ((int64_t)h * hd.wide_chunks + gr.chunk0 + ch + x0) * WIDE_ROWS + wr;
-    w_step = WIDE_ROWS / halves;
-    total += (x1 - x0 + 1) * halves;
+    const int T = wide_tokens(G);
+    ch = (t - gr.tok0) / T;
+    wr = ((t - gr.tok0) - ch * T) * G + g;
+    weight = ws.weight(ch, G);
+    halves = weight == 1 ? 2 : 1;
+    x0 = (h_cost + ws.before(0, ch)) / hd.wide_each;
+    const int x1 = (h_cost + ws.before(0, ch) + (ws.tiles_of(0) - 1) * weight) / hd.wide_each;
+    total += halves * (ws.stripes == 1 ? x1 - x0 + 1 : 2 * ws.stripes);
   }
-  auto entry = [&](int k) {
-    if (k >= total) return make_float2(-INFINITY, 0.0f);
-    return k < n_parts ? __ldcg(a.w.narrow_ml + n_row + k * NARROW_ROWS) : __ldcg(a.w.wide_ml + w_row + (int64_t)(k - n_parts) * w_step);
+  // where part k of the row lies (in rows; the prefixes' behind all narrow ones), -1: nowhere
+  auto place = [&](int k) -> int64_t {
+    if (k >= total) return -1;
+    if (k < n_parts) return n_row + k * NARROW_ROWS;
+    k -= n_parts;
+    const int half = halves == 2 ? k & 1 : 0;
+    if (halves == 2) k >>= 1;
+    int stripe = 0, cta = x0 + k;
+    if (ws.stripes > 1) {
+      stripe = k >> 1;
+      const int at = h_cost + ws.before(stripe, ch), from = at / hd.wide_each;
+      cta = from + (k & 1);
+      if (cta > (at + (ws.tiles_of(stripe) - 1) * weight) / hd.wide_each) return -1;
+    }
+    return a.w.wide_row0 + ((int64_t)h * hd.wide_chunks + gr.chunk0 + stripe * ws.chunks + ch + cta) * WIDE_ROWS + half * (WIDE_ROWS / 2) + wr;
   };
-  auto result = [&](int k) {
-    const float* p = k < n_parts ? a.w.narrow_o + (n_row + k * NARROW_ROWS) * 128 : a.w.wide_o + (w_row + (int64_t)(k - n_parts) * w_step) * 128;
-    return __ldcg(reinterpret_cast<const float4*>(p) + lane);
-  };
-  float2 e = entry(lane);
-  float4 v[8];
-#pragma unroll
-  for (int q = 0; q < 8; ++q)
-    if (sub + q * WARPS < total) v[q] = result(sub + q * WARPS);
-  float top = e.x;
-  for (int k = lane + 32; k < total; k += 32) top = fmaxf(top, entry(k).x);
-#pragma unroll
-  for (int off = 16; off; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-  const float ref = top == -INFINITY ? 0.0f : top;
-  float sum = 0.0f;
+  float top = -INFINITY, sum = 0.0f;
   float4 acc = make_float4(0, 0, 0, 0);
+  // up to 32 parts at a time (more than that are joined to what is there, as the parts themselves were)
   for (int k0 = 0; k0 < total; k0 += 32) {
-    if (k0) e = entry(k0 + lane);
-    const float f = ex2(e.x - ref);
-    sum += e.y * f;
+    const int64_t at = place(k0 + lane);
+    const float2 e = at >= 0 ? __ldcg(a.w.ml + at) : make_float2(-INFINITY, 0.0f);
     const int m = min(32, total - k0);
-    for (int b = 0; b < 32 && b < m; b += 8 * WARPS) {
-      if (k0 + b) {
+    float mx = e.x;
+    float4 v[8];
+    auto load = [&](int b) {
 #pragma unroll
-        for (int q = 0; q < 8; ++q)
-          if (b + sub + q * WARPS < m) v[q] = result(k0 + b + sub + q * WARPS);
+      for (int q = 0; q < 8; ++q) {
+        const int k = b + sub + q * WARPS;
+        const int64_t from = __shfl_sync(0xffffffffu, at, k & 31);
+        v[q] = k < m && from >= 0 ? __ldcg(reinterpret_cast<const float4*>(a.w.o + from * 128) + lane) : make_float4(0, 0, 0, 0);
       }
+    };
+    load(0);
+#pragma unroll
+    for (int off = 16; off; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
+    const float was = top;
+    top = fmaxf(top, mx);
+    const float ref = top == -INFINITY ? 0.0f : top, f = ex2(e.x - ref);
+    if (k0) {
+      const float back = ex2(was - ref);
+      sum *= back;
+      acc.x *= back; acc.y *= back; acc.z *= back; acc.w *= back;
+    }
+    sum += e.y * f;
+    for (int b = 0; b < m; b += 8 * WARPS) {
+      if (b) load(b);
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         const int k = b + sub + q * WARPS;
@@ -355,6 +391,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
       }
     }
   }
+  const float ref = top == -INFINITY ? 0.0f : top;
 #pragma unroll
   for (int off = 16; off; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
   if (WARPS > 1) {
@@ -382,7 +419,9 @@ AttendLayout layout_of(int sm_count, int n_kv_heads, int n_seqs, int n_tokens, i
   int64_t narrow = n_tokens * G / NARROW_ROWS + n_seqs;
   if (narrow > n_tokens * per_token) narrow = n_tokens * per_token;
   const int64_t wide = n_tokens / wide_tokens((int)G) + n_seqs / 2 + 1;
-  const size_t narrow_slots = (size_t)(H * narrow + l.narrow_grid), wide_slots = (size_t)(H * wide + l.wide_grid);
+  // (chunks of stripes, where there are several: a stripe is at least half a CTA's cost long and a chunk's tile costs at least
+  // 3/2 on average, so that there are 4/3 as many as CTAs at most, and one more for every chunk)
+  const size_t narrow_slots = (size_t)(H * narrow + l.narrow_grid), wide_slots = (size_t)(H * wide + 3 * l.wide_grid);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = asl_align256(off + bytes); return at; };
   l.head = take(sizeof(AttendHead));
@@ -392,10 +431,9 @@ AttendLayout layout_of(int sm_count, int n_kv_heads, int n_seqs, int n_tokens, i
   l.tok_seq = take(sizeof(int2) * n_tokens);
   l.narrow_start = take(sizeof(AttendStart) * l.narrow_grid);
   l.wide_start = take(sizeof(AttendStart) * l.wide_grid);
-  l.narrow_ml = take(sizeof(float2) * NARROW_ROWS * narrow_slots);
-  l.narrow_o = take(sizeof(float) * 128 * NARROW_ROWS * narrow_slots);
-  l.wide_ml = take(sizeof(float2) * WIDE_ROWS * wide_slots);
-  l.wide_o = take(sizeof(float) * 128 * WIDE_ROWS * wide_slots);
+  l.wide_row0 = (int64_t)(NARROW_ROWS * narrow_slots);
+  l.ml = take(sizeof(float2) * (l.wide_row0 + WIDE_ROWS * wide_slots));
+  l.o = take(sizeof(float) * 128 * (l.wide_row0 + WIDE_ROWS * wide_slots));
   l.total = off;
   return l;
 }
@@ -410,10 +448,9 @@ AttendPtrs ptrs_of(const AttendLayout& l, void* workspace) {
   p.tok_seq = reinterpret_cast<int2*>(w + l.tok_seq);
   p.narrow_start = reinterpret_cast<AttendStart*>(w + l.narrow_start);
   p.wide_start = reinterpret_cast<AttendStart*>(w + l.wide_start);
-  p.narrow_ml = reinterpret_cast<float2*>(w + l.narrow_ml);
-  p.narrow_o = reinterpret_cast<float*>(w + l.narrow_o);
-  p.wide_ml = reinterpret_cast<float2*>(w + l.wide_ml);
-  p.wide_o = reinterpret_cast<float*>(w + l.wide_o);
+  p.ml = reinterpret_cast<float2*>(w + l.ml);
+  p.o = reinterpret_cast<float*>(w + l.o);
+  p.wide_row0 = l.wide_row0;
   return p;
 }
 

@@ -5,7 +5,9 @@
 //           64 keys; per kv head sum over sequences of chunks x tiles.
 //   wide    the prefixes that groups of neighbours share, [0, pfx): chunks of up to 256 rows of the group, tiles of 128 keys
 //           that count 2 where a chunk has more than 128 rows (both halves multiply) and 1 else (the halves take keys in turn).
-// A CTA's stretch of a chunk is a part; parts of a chunk have the running maximum, the sum and the unnormalised result of
+//           Where a group has several chunks its keys are cut into stripes of about a CTA's stretch, and a stripe's chunks come
+//           one behind another: CTAs that read the same keys do so at the same time, once from HBM and then from L2.
+// A CTA's stretch of a chunk (of a stripe) is a part; parts of a chunk have the running maximum, the sum and the unnormalised result of
 // their keys, and lie at (number of the chunk + number of the CTA): either grows by one from part to part.
 #pragma once
 #include "pages.cuh"
@@ -26,17 +28,18 @@ struct __align__(16) AttendSeq {
 };
 struct __align__(16) AttendGroup {
   int32_t tok0, ntok, slot, pfx;
-  int32_t cost0, chunk0, pad0, pad1;   // wide cost and chunks before
+  int32_t cost0, chunk0, stripe, pad0; // wide cost and chunks (of stripes) before; tiles of a stripe
 };
 // Where a CTA's stretch begins (h < 0: it has none), with all that it needs to know there: one round trip to memory.
 struct __align__(16) AttendStart {
   int32_t h, item, chunk, tile;
   union { AttendSeq seq; AttendGroup group; };
-  int32_t items, total, chunks, each;  // sequences or groups; tiles or cost, and chunks, per kv head; per CTA
+  int32_t items, total, chunks, more;  // sequences or groups; tiles or cost, and chunks, per kv head; tiles per CTA, or the stripe
 };
 
 struct AttendLayout {      // byte offsets in the workspace
-  size_t head, seqs, groups, same, tok_seq, narrow_start, wide_start, narrow_ml, narrow_o, wide_ml, wide_o, total;
+  size_t head, seqs, groups, same, tok_seq, narrow_start, wide_start, ml, o, total;
+  int64_t wide_row0;
   int32_t narrow_grid, wide_grid;
 };
 
@@ -48,10 +51,9 @@ struct AttendPtrs {
   int2* tok_seq;           // [n_tokens] a token's entry (-1: nobody's) and group
   AttendStart* narrow_start;
   AttendStart* wide_start;
-  float2* narrow_ml;       // [slot][16] (maximum in powers of two, sum)
-  float* narrow_o;         // [slot][16][128]
-  float2* wide_ml;         // [slot][256]
-  float* wide_o;           // [slot][256][128]
+  float2* ml;              // of every part's rows: 16 of a narrow slot, then, from wide_row0 on, 256 of a wide one:
+  float* o;                // (maximum in powers of two, sum); [128] unnormalised result
+  int64_t wide_row0;
 };
 
 struct AttendArgs {
@@ -67,7 +69,7 @@ struct AttendArgs {
   float scale_log2;
 };
 
-// Chunks of a group's rows: as many tokens as fill 256 rows, dealt out evenly.
+// Tokens of a chunk of a group's rows (at least two, since a token has at most 128).
 #ifdef __CUDACC__
 __host__
 __device__
@@ -93,17 +95,26 @@ __device__ __forceinline__ bool plan_fits(const AttendArgs& a, const AttendHead&
   if (!fits && threadIdx.x == 0) note_error(a.g.err, ASL_ERR_WORKSPACE, -1);
   return fits;
 }
-// cost of a tile of the chunk that begins at token `t` of its group
-__device__ __forceinline__ int wide_weight(const AttendGroup& gr, int chunk, int G) {
-  const int T = wide_tokens(G), n = min(T, gr.ntok - chunk * T);
-  return n * G > WIDE_ROWS / 2 ? 2 : 1;
-}
-__device__ __forceinline__ int wide_group_cost(int ntok, int pfx, int G) {      // of all its chunks
-  const int T = wide_tokens(G), tiles = (pfx + WIDE_KEYS - 1) / WIDE_KEYS;
-  const int whole = ntok / T, rest = ntok % T;
-  const int w = T * G > WIDE_ROWS / 2 ? 2 : 1;
-  return tiles * (whole * w + (rest ? (rest * G > WIDE_ROWS / 2 ? 2 : 1) : 0));
-}
+// A group's tiles, chunks and cost.  All chunks but the last have as many tokens as fit (and more than 128 rows).
+struct WideShape {
+  int tiles, whole, rest, chunks, stripe, stripes;
+  int sum;                                 // cost of one tile of every chunk
+  __device__ __forceinline__ WideShape(int ntok, int pfx, int G, int stripe_) {
+    const int T = wide_tokens(G);
+    tiles = (pfx + WIDE_KEYS - 1) / WIDE_KEYS;
+    whole = ntok / T;
+    rest = ntok - whole * T;
+    chunks = whole + (rest > 0);
+    sum = 2 * whole + (rest ? weight_of(rest, G) : 0);
+    stripe = chunks > 1 ? stripe_ : tiles;
+    stripes = tiles ? (tiles + stripe - 1) / stripe : 0;
+  }
+  static __device__ __forceinline__ int weight_of(int tokens, int G) { return tokens * G > WIDE_ROWS / 2 ? 2 : 1; }
+  __device__ __forceinline__ int weight(int chunk, int G) const { return chunk < whole ? 2 : weight_of(rest, G); }
+  __device__ __forceinline__ int tiles_of(int s) const { return min(stripe, tiles - s * stripe); }
+  // cost before a chunk of a stripe
+  __device__ __forceinline__ int before(int s, int chunk) const { return s * stripe * sum + tiles_of(s) * 2 * chunk; }
+};
 __device__ __forceinline__ AttendStart load_start(const AttendStart* s) {
   AttendStart r;
 #pragma unroll

@@ -53,7 +53,7 @@ struct Walk {
     if (!plan_fits(a, hd) || st.h < 0) return false;
     h = st.h; i = st.item; chunk = st.chunk; tile = st.tile;
     s = st.seq;
-    items = st.items; total = st.total; chunks = st.chunks; each = st.each;
+    items = st.items; total = st.total; chunks = st.chunks; each = st.more;
     left = min(each, a.g.n_kv_heads * total - (int)blockIdx.x * each);
     sizes(a);
     return true;
@@ -346,8 +346,8 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
               *reinterpret_cast<uint2*>(a.out + row * 128 + hc) = v;
               if (a.lse && half == 0 && ch == 0) a.lse[row] = (at + log2f(sum)) * 0.6931471805599453f;
             } else {
-              *reinterpret_cast<float4*>(a.w.narrow_o + (slot * NARROW_ROWS + r) * 128 + hc) = acc;
-              if (half == 0 && ch == 0) a.w.narrow_ml[slot * NARROW_ROWS + r] = make_float2(top, sum);
+              *reinterpret_cast<float4*>(a.w.o + (slot * NARROW_ROWS + r) * 128 + hc) = acc;
+              if (half == 0 && ch == 0) a.w.ml[slot * NARROW_ROWS + r] = make_float2(top, sum);
             }
           }
         }

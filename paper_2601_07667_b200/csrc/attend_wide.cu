@@ -27,57 +27,64 @@ struct WideSmem {
   static constexpr int CODES = V + V_RING * TILE_BYTES;             // E4M3 tiles as they come
   static constexpr int BARS = CODES + (FP8 ? 2 * TILE_HALF : 0);
   static constexpr int KF = 0, KE = KF + K_RING, VF = KE + K_RING, VE = VF + 3, SF = VE + 3, PF = SF + 2, OD = PF + 2, QF = OD + 2,
-                       QE = QF + 1, CF = QE + 1, CE = CF + 2, DRAIN = CE + 2, N_BARS = DRAIN + 1;
+                       QE = QF + 1, CF = QE + 1, CE = CF + 2, DRAIN = CE + 2, N_BARS = DRAIN + 2;
   static constexpr int MISC = BARS + 256;
   static constexpr int BYTES = MISC + 16 + 1024;
   static constexpr int THREADS = FP8 ? 512 : 384;
   // Registers a thread: a row of 128 logits stays in them.  Launched with REGS each; the warpgroups' shares are no more together.
-  static constexpr int REGS = FP8 ? 128 : 168, REGS_FEW = FP8 ? 56 : 72, REGS_ROWS = FP8 ? 200 : 216;
+  static constexpr int REGS = FP8 ? 128 : 168, REGS_FEW = FP8 ? 64 : 72, REGS_ROWS = FP8 ? 192 : 216;
   static_assert(REGS * THREADS >= REGS_FEW * (THREADS - 256) + REGS_ROWS * 256, "a warpgroup would wait for registers");
   static_assert(N_BARS * 8 <= 256 && BYTES <= 232448, "shared memory budget of one CTA");
 };
 
-// A CTA's stretch: chunk by chunk the tiles tile .. end - 1.
+// A CTA's stretch: chunk by chunk (of a stripe) the tiles tile .. end - 1.
 struct Walk {
-  int h, gi, chunk, tile, end;
-  int nt, weight, rows, items, total, chunks;
+  int h, gi, stripe, chunk, tile, end;
+  int weight, rows, items, total, chunks;
   int stop;                                // cost at which the stretch ends
+  int n_chunks;                            // of the group
   AttendGroup g;
-  __device__ __forceinline__ bool set(const AttendArgs& a) {        // a chunk of group g: its tiles in the stretch
-    const int T = wide_tokens(a.group_heads);
-    nt = (g.pfx + WIDE_KEYS - 1) / WIDE_KEYS;
-    weight = wide_weight(g, chunk, a.group_heads);
-    rows = min(T, g.ntok - chunk * T) * a.group_heads;
-    const int w0 = T * a.group_heads > WIDE_ROWS / 2 ? 2 : 1;
-    const int at = h * total + g.cost0 + chunk * nt * w0;
-    end = min(nt, (stop - at + weight - 1) / weight);
+  __device__ __forceinline__ bool set(const AttendArgs& a, bool begins) {
+    const int G = a.group_heads, T = wide_tokens(G);
+    const WideShape w(g.ntok, g.pfx, G, g.stripe);
+    const int t0 = stripe * w.stripe, nt = w.tiles_of(stripe), at = h * total + g.cost0 + w.before(stripe, chunk);
+    weight = w.weight(chunk, G);
+    rows = min(T, g.ntok - chunk * T) * G;
+    if (begins) tile = t0;
+    end = min(t0 + nt, t0 + (stop - at + weight - 1) / weight);
+    n_chunks = w.chunks;
     return end > tile;
   }
   __device__ __forceinline__ bool begin(const AttendArgs& a) {
     const AttendHead hd = load_head(a.w.head);
     const AttendStart st = load_start(a.w.wide_start + blockIdx.x);
     if (!plan_fits(a, hd) || st.h < 0) return false;
-    h = st.h; gi = st.item; chunk = st.chunk; tile = st.tile;
+    h = st.h; gi = st.item; chunk = st.chunk; tile = st.tile; stripe = st.more;
     g = st.group;
     items = st.items; total = st.total; chunks = st.chunks;
-    stop = min(a.g.n_kv_heads * total, ((int)blockIdx.x + 1) * st.each);
-    return set(a) || next(a);
+    stop = min(a.g.n_kv_heads * total, ((int)blockIdx.x + 1) * hd.wide_each);
+    return set(a, false) || next(a);
   }
   __device__ __forceinline__ bool next(const AttendArgs& a) {
-    tile = 0;
-    ++chunk;
-    while (g.pfx == 0 || chunk * wide_tokens(a.group_heads) >= g.ntok) {
+    if (++chunk == n_chunks) {
       chunk = 0;
-      if (++gi >= items) {
-        gi = 0;
-        if (++h >= a.g.n_kv_heads) return false;
+      ++stripe;
+      if (n_chunks == 1 || stripe * g.stripe * WIDE_KEYS >= g.pfx) {
+        stripe = 0;
+        do {
+          if (++gi >= items) {
+            gi = 0;
+            if (++h >= a.g.n_kv_heads) return false;
+          }
+          g = load_group(a.w.groups + gi);
+        } while (g.pfx == 0);
       }
-      g = load_group(a.w.groups + gi);
     }
-    return set(a);
+    return set(a, true);
   }
   __device__ __forceinline__ bool full() const { return weight == 2; }
   __device__ __forceinline__ int keys(int t) const { return min(WIDE_KEYS, g.pfx - t * WIDE_KEYS); }
+  __device__ __forceinline__ int64_t slot() const { return (int64_t)h * chunks + g.chunk0 + stripe * n_chunks + chunk + blockIdx.x; }
 };
 
 __device__ __forceinline__ float max3(float a, float b, float c) {        // NaN where one is
@@ -117,8 +124,9 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   volatile int* s_abort = reinterpret_cast<volatile int*>(sm + S::MISC + 8);
   auto bar = [&](int i) { return base + S::BARS + 8 * i; };
   if (threadIdx.x == 0) {
-    for (int i = 0; i < K_RING; ++i) { mbar_init(bar(S::KF + i), FP8 ? 128 : 1); mbar_init(bar(S::KE + i), 1); }
-    for (int i = 0; i < S::V_RING; ++i) { mbar_init(bar(S::VF + i), 1); mbar_init(bar(S::VE + i), 1); }
+    // (tiles and queries are given back by both issuing warps)
+    for (int i = 0; i < K_RING; ++i) { mbar_init(bar(S::KF + i), FP8 ? 128 : 1); mbar_init(bar(S::KE + i), 2); }
+    for (int i = 0; i < S::V_RING; ++i) { mbar_init(bar(S::VF + i), 1); mbar_init(bar(S::VE + i), 2); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(S::SF + i), 1);
       mbar_init(bar(S::PF + i), 4);
@@ -127,8 +135,9 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       mbar_init(bar(S::CE + i), 128);
     }
     mbar_init(bar(S::QF), 1);
-    mbar_init(bar(S::QE), 1);
+    mbar_init(bar(S::QE), 2);
     mbar_init(bar(S::DRAIN), 1);
+    mbar_init(bar(S::DRAIN + 1), 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -231,8 +240,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       }
       if (!ok) break;
       // the part: this stream's rows of the run
-      const int64_t slot = (int64_t)w.h * w.chunks + w.g.chunk0 + w.chunk + blockIdx.x;
-      const int64_t at = slot * WIDE_ROWS + s * 128 + row;
+      const int64_t at = a.w.wide_row0 + w.slot() * WIDE_ROWS + s * 128 + row;
       if (t0 < w.end) {
         if (!__all_sync(0xffffffffu, mbar_wait(bar(S::OD + s), (it - 1) & 1, s_abort, 233, true))) { ok = false; break; }
         tc_fence_after();
@@ -244,7 +252,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             tc_ld_wait(o[k & 1]);
             if (k < 7) tc_ld_lane(ot + 16 * (k + 1), o[(k + 1) & 1]);
             if (r < w.rows) {
-              float4* to = reinterpret_cast<float4*>(a.w.wide_o + at * 128 + 16 * k);
+              float4* to = reinterpret_cast<float4*>(a.w.o + at * 128 + 16 * k);
 #pragma unroll
               for (int e = 0; e < 4; ++e)
                 to[e] = make_float4(__uint_as_float(o[k & 1][4 * e]), __uint_as_float(o[k & 1][4 * e + 1]), __uint_as_float(o[k & 1][4 * e + 2]),
@@ -254,7 +262,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           tc_fence_before();
         }
       }
-      if (r < w.rows) a.w.wide_ml[at] = make_float2(t0 < w.end ? m : -INFINITY, hsum(l2));
+      if (r < w.rows) a.w.ml[at] = make_float2(t0 < w.end ? m : -INFINITY, hsum(l2));
       more = w.next(a);
     }
   } else {
@@ -329,83 +337,83 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         }
         mbar_wait(bar(S::QF), (run - 1) & 1, s_abort, 216, false);
       }
-    } else if (any && warp == 1) {
+    } else if (any && warp <= 2) {
       // =============================== products ===================================
+      // A warp per stream, so that one's waits are filled by the other's products (one warp for both: 3600 clk a tile of 256
+      // rows, of which 800 passed in waits with the tensor pipe empty).
       // (What the products' operands follow from is shuffled, so that the compiler knows it to be the same in all lanes and
       // keeps descriptors in uniform registers: moved there one by one they cost 100 clk a product instead of 64.)
-      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      const int s = __shfl_sync(0xffffffffu, warp - 1, 0);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0) + s * 128;
       const uint32_t id_full = instr_desc(128, WIDE_KEYS), id_pv = instr_desc(128, 128) | B_MN_MAJOR;
       int n = 0;                           // tiles before this run
-      uint32_t pv[2] = {0, 0};             // parity of each stream's next product P V
+      uint32_t pv = 0;                     // parity of the next product P V
       bool ok = true, more = true;
       for (int run = 0; ok && more; ++run) {
         const bool full = __shfl_sync(0xffffffffu, (int)w.full(), 0);
         const int tile = __shfl_sync(0xffffffffu, w.tile, 0), nt = __shfl_sync(0xffffffffu, w.end, 0) - tile;
         const int pfx = __shfl_sync(0xffffffffu, w.g.pfx, 0) - tile * WIDE_KEYS;      // keys from the first tile on
-        const int items = full ? 2 * nt : nt;
-        auto keys_here = [&](int i) {      // the tile of item i's keys
-          const int j = full ? i >> 1 : i, ks = (n + j) % K_RING;
-          if (ok && i < items && (!full || !(i & 1)))
-            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::KF + ks), ((n + j) / K_RING) & 1, s_abort, 221, true));
+        const int first = full ? 0 : s, step = full ? 1 : 2;                          // the stream's tiles
+        auto keys_here = [&](int j) {
+          if (ok && j < nt) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::KF + (n + j) % K_RING), ((n + j) / K_RING) & 1, s_abort, 221, true));
         };
-        auto values_here = [&](int i) {
-          const int j = full ? i >> 1 : i, vs = (n + j) % S::V_RING;
-          if (ok && i < items && (!full || !(i & 1)))
-            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + vs), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+        auto values_here = [&](int j) {
+          if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + (n + j) % S::V_RING), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
         };
-        auto scores = [&](int i) {         // S of item i
-          const int j = full ? i >> 1 : i, s = i & 1, ks = (n + j) % K_RING, left = pfx - j * WIDE_KEYS;
+        auto scores = [&](int j) {         // S of tile j
+          const int ks = (n + j) % K_RING, left = pfx - j * WIDE_KEYS;
           const uint64_t qd = smem_desc(base + (full ? s : 0) * 128 * 128), kd = smem_desc(base + S::K + ks * TILE_BYTES);
           const uint32_t id = left >= WIDE_KEYS ? id_full : instr_desc(128, left);
           if (elect_one()) {
 #pragma unroll
             for (int x = 0; x < 8; ++x)
-              tc_mma(tm + s * 128, qd + ((x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2), kd + ((x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2), id, x > 0);
+              tc_mma(tm, qd + ((x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2), kd + ((x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2), id, x > 0);
             tc_commit(bar(S::SF + s));
-            if (!full || s == 1) tc_commit(bar(S::KE + ks));
-            if (i + 1 == items) tc_commit(bar(S::QE));
+            tc_commit(bar(S::KE + ks));
+            if (!full) tc_commit(bar(S::KE + ks));                  // nobody else reads it
+            if (j + step >= nt) tc_commit(bar(S::QE));
           }
           __syncwarp();
         };
         ok = __all_sync(0xffffffffu, mbar_wait(bar(S::QF), run & 1, s_abort, 222, true));
-        keys_here(0);
-        tc_fence_after();
-        if (ok) scores(0);
-        keys_here(1);
-        if (ok && items > 1) scores(1);
-        for (int i = 0; ok && i < items; ++i) {
-          const int j = full ? i >> 1 : i, s = i & 1, vs = (n + j) % S::V_RING, left = pfx - j * WIDE_KEYS;
-          // (tiles are waited for before the weights, while the tensor pipe still has products of the item before)
-          values_here(i);
-          keys_here(i + 2);
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv[s], s_abort, 223, true));
+        keys_here(first);
+        if (ok && first < nt) {
+          tc_fence_after();
+          scores(first);
+        } else if (ok && lane == 0) {
+          mbar_arrive(bar(S::QE));         // a run of one tile: the other stream's
+        }
+        for (int j = first; ok && j < nt; j += step) {
+          const int vs = (n + j) % S::V_RING, left = pfx - j * WIDE_KEYS;
+          values_here(j);                  // (tiles are waited for before the weights, while the pipe still has products)
+          keys_here(j + step);
+          ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv, s_abort, 223, true));
           if (!ok) break;
           tc_fence_after();
           const uint64_t vd = smem_desc_mn(base + S::V + vs * TILE_BYTES, TILE_HALF);
-          const uint32_t fresh = i < 2;    // the stream's first product of the run
+          const uint32_t old = j > first;  // there is a result to add to
           if (elect_one()) {
             if (left >= WIDE_KEYS) {
 #pragma unroll
-              for (int x = 0; x < 8; ++x)
-                tc_mma_ts(tm + 256 + s * 128, tm + s * 128 + x * 8, vd + x * (2048 >> 4), id_pv, x > 0 ? 1u : fresh ^ 1u);
+              for (int x = 0; x < 8; ++x) tc_mma_ts(tm + 256, tm + x * 8, vd + x * (2048 >> 4), id_pv, x > 0 ? 1u : old);
             } else {
-              for (int x = 0; x < left >> 4; ++x)
-                tc_mma_ts(tm + 256 + s * 128, tm + s * 128 + x * 8, vd + x * (2048 >> 4), id_pv, x > 0 ? 1u : fresh ^ 1u);
+              for (int x = 0; x < left >> 4; ++x) tc_mma_ts(tm + 256, tm + x * 8, vd + x * (2048 >> 4), id_pv, x > 0 ? 1u : old);
             }
             tc_commit(bar(S::OD + s));
-            if (!full || s == 1) tc_commit(bar(S::VE + vs));
+            tc_commit(bar(S::VE + vs));
+            if (!full) tc_commit(bar(S::VE + vs));
           }
           __syncwarp();
-          pv[s] ^= 1u;
-          if (i + 2 < items) scores(i + 2);
+          pv ^= 1u;
+          if (j + step < nt) scores(j + step);
         }
         n += nt;
         if (ok) more = w.next(a);
       }
       if (!ok) {                           // nothing writes tensor memory when it is freed
         if (elect_one()) {
-          tc_commit(bar(S::DRAIN));
-          mbar_wait(bar(S::DRAIN), 0, s_abort, 225, false);
+          tc_commit(bar(S::DRAIN + s));
+          mbar_wait(bar(S::DRAIN + s), 0, s_abort, 225, false);
         }
         __syncwarp();
       }
