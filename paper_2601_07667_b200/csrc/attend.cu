@@ -8,9 +8,10 @@ namespace {
 
 constexpr int PLAN_THREADS = 512;
 constexpr int NARROW_CTAS = 2;             // per SM
-// Least keys that a prefix saves (its length times all its readers but one) for it to be read by the group: below, one more
-// launch with work and one more part per row cost more than the copies of it in L2.
-constexpr int SHARE_MIN_KEYS = 1024;
+// Least bytes of K and V that the groups' prefixes save (each its length times all its readers but one) for them to be read by
+// groups: below, one more kernel and one more part per row cost more than the copies out of L2.
+constexpr float SHARE_MIN_BYTES = 32e6f;
+constexpr int64_t SAME_INSIDE = 16384;     // entries of the batch's rows of the table that the plan's own block compares
 
 // Leading pages that an entry of the batch has in common with the one before it; only pages that both hold in full.
 constexpr int SAME_THREADS = 256, SAME_EACH = 8;
@@ -72,79 +73,101 @@ struct PlanArgs {
   PagePool g;
   asl_batch b;
   AttendPtrs w;
-  int32_t G, n_q_heads, share, narrow_grid, wide_grid;
+  int32_t G, n_q_heads, narrow_grid, wide_grid;
+  int32_t share;           // 0: nothing is; what neighbours have in common comes from 1: attend_same_kernel, 2: the plan itself
 };
 
-// One block: groups of neighbours, prefix sums over sequences and groups, and where every CTA's stretch begins.
+// One block: groups of neighbours, prefix sums over sequences and groups, and where every CTA's stretch begins.  All of it in
+// shared memory: what bounds it is the chain of its steps (two loads, the groups' walk of some 30 clk an entry, four prefix sums).
 __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   extern __shared__ int32_t sm[];
   __shared__ int part[PLAN_THREADS / 32];
   __shared__ int n_groups_s, any_full;
   __shared__ unsigned long long most_s;
   pdl_wait_predecessor();
-  const int tid = threadIdx.x, n = a.b.n_seqs, G = a.G;
-  int32_t* ntok = sm;
+  const int tid = threadIdx.x, n = a.b.n_seqs, G = a.G, H = a.g.n_kv_heads;
+  int32_t* ntok = sm;                      // per entry
   int32_t* len = sm + n;
-  int32_t* grp = sm + 2 * n;
-  int32_t* first = sm + 3 * n;             // [n + 1] narrow tiles before; until the groups are known: tokens in common
-  int32_t* gpfx = first + n + 1;           // per group: shared tokens, first entry, wide cost before
-  int32_t* gat = gpfx + n;
-  int32_t* gcost = gat + n;                // [n + 1]
+  int32_t* slot = sm + 2 * n;
+  int32_t* tok0 = sm + 3 * n;
+  int32_t* grp = sm + 4 * n;
+  int32_t* com = sm + 5 * n;               // shared tokens with the entry before; then narrow chunks before
+  int32_t* gpfx = sm + 6 * n;              // per group: shared tokens, first entry, tokens, chunks of stripes before
+  int32_t* gat = sm + 7 * n;
+  int32_t* gtok = sm + 8 * n;
+  int32_t* gchunk = sm + 9 * n;
+  int32_t* first = sm + 10 * n;            // [n + 1] narrow tiles before
+  int32_t* gcost = sm + 11 * n + 1;        // [n + 1] wide cost before
   if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; }
-  __syncthreads();
   for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tok_seq[t] = make_int2(-1, -1);
+  __syncthreads();
   for (int i = tid; i < n; i += PLAN_THREADS) {
     const int s = __ldcg(a.b.slots + i), t0 = __ldcg(a.b.cu_q + i), t1 = __ldcg(a.b.cu_q + i + 1);
+    const int same = a.share == 1 ? __ldcg(a.w.same + i) : 0;
     const bool slot_ok = (unsigned)s < (unsigned)a.g.max_seqs, tok_ok = t0 >= 0 && t1 >= t0 && t1 <= a.b.n_tokens;
+    const int l = slot_ok ? __ldcg(a.g.len + s) : 0;
     if (slot_ok && !tok_ok) note_error(a.g.err, ASL_ERR_INVALID, s);
-    ntok[i] = slot_ok && tok_ok ? t1 - t0 : 0;
-    len[i] = ntok[i] ? min(max(__ldcg(a.g.len + s), 0), a.g.max_pages << a.g.page_shift) : 0;
-    first[i] = a.share ? __ldcg(a.w.same + i) << a.g.page_shift : 0;
+    const int m = slot_ok && tok_ok ? t1 - t0 : 0;
+    ntok[i] = m;
+    slot[i] = m ? s : -1;
+    tok0[i] = t0;
+    len[i] = m ? min(max(l, 0), a.g.max_pages << a.g.page_shift) : 0;
+    com[i] = same << a.g.page_shift;
     // tiles, were nothing shared: they are counted in 32 bits
-    if (ntok[i]) atomicAdd(&most_s, (unsigned long long)narrow_chunks_of(ntok[i], G) * (unsigned)(len[i] / NARROW_KEYS + 2));
+    if (m) atomicAdd(&most_s, (unsigned long long)narrow_chunks_of(m, G) * (unsigned)(len[i] / NARROW_KEYS + 2));
   }
   __syncthreads();
-  if (most_s * a.g.n_kv_heads >= 1ull << 30) {
+  if (most_s * H >= 1ull << 30) {
     if (tid == 0) note_error(a.g.err, ASL_ERR_UNSUPPORTED, -1);
     return;
   }
-  // Groups: an entry joins the group before it where that group then saves no less than without it.  One warp, 32 entries in
-  // its lanes, all of whose threads walk them together.
-  if (tid < 32) {
-    int ng = 0, held = 0, keys = 0;                          // of the open group: entries (0: none is open), shared tokens
-    auto close = [&]() { if (held && tid == 0) gpfx[ng - 1] = held > 1 && (int64_t)(held - 1) * keys >= SHARE_MIN_KEYS ? keys : 0; };
-    for (int i0 = 0; i0 < n; i0 += 32) {
-      const int i = i0 + tid;
-      int mine = 0, own = 0, com = 0, group = -1;
-      if (i < n) {
-        mine = ntok[i];
-        own = max(0, len[i] - ntok[i]) >> a.g.page_shift << a.g.page_shift;        // all its tokens see these
-        com = min(own, first[i]);
-      }
-      for (int j = 0; j < min(32, n - i0); ++j) {
-        const int has = __shfl_sync(0xffffffffu, mine, j), o = __shfl_sync(0xffffffffu, own, j), c = __shfl_sync(0xffffffffu, com, j);
-        if (!has) {
-          close();
-          held = 0;
-          continue;
+  if (a.share == 2) {                      // few pages: no launch of its own for what neighbours have in common, a warp a pair
+    for (int i = 1 + (tid >> 5); i < n; i += PLAN_THREADS / 32) {
+      int m = min(len[i], len[i - 1]) >> a.g.page_shift;
+      const int32_t* x = a.g.table + (int64_t)slot[i] * a.g.max_pages;
+      const int32_t* y = a.g.table + (int64_t)slot[i - 1] * a.g.max_pages;
+      for (int j0 = 0; j0 < m; j0 += 128) {
+        int u[4], v[4], at = m;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int j = j0 + q * 32 + (tid & 31);
+          u[q] = j < m ? __ldcg(x + j) : 0;
+          v[q] = j < m ? __ldcg(y + j) : 0;
         }
-        const int both = min(keys, c);
-        if (held && both > 0 && (int64_t)held * both >= (int64_t)(held - 1) * keys) {
-          keys = both;
-          ++held;
-        } else {
-          close();
-          if (tid == 0) gat[ng] = i0 + j;
-          ++ng;
-          held = 1;
-          keys = o;
-        }
-        if (tid == j) group = ng - 1;
+#pragma unroll
+        for (int q = 3; q >= 0; --q)
+          if (u[q] != v[q]) at = j0 + q * 32 + (tid & 31);
+        m = min(m, __reduce_min_sync(0xffffffffu, at));
       }
-      if (i < n) grp[i] = group;
+      if ((tid & 31) == 0) com[i] = max(m, 0) << a.g.page_shift;
     }
-    close();
-    if (tid == 0) n_groups_s = ng;
+    __syncthreads();
+  }
+  // Groups: an entry joins the group before it where that group then saves no less than without it.
+  if (tid == 0) {
+    int ng = 0, held = 0, keys = 0;                          // of the open group: entries (0: none is open), shared tokens
+    float saved = 0.0f;                                      // keys read less often, by all groups so far
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const int has = ntok[i], own = max(0, len[i] - has) >> a.g.page_shift << a.g.page_shift;     // all its tokens see these
+      const int both = min(keys, min(own, com[i]));
+      const bool joins = has && held && both > 0 && (float)held * both >= (float)(held - 1) * keys;
+      if (!joins && held) {
+        gpfx[ng - 1] = held > 1 ? keys : 0;
+        saved += (float)(held - 1) * keys;
+      }
+      if (!joins && has) gat[ng++] = i;
+      held = has ? (joins ? held + 1 : 1) : 0;
+      keys = joins ? both : own;
+      grp[i] = has ? ng - 1 : -1;
+    }
+    if (held) {
+      gpfx[ng - 1] = held > 1 ? keys : 0;
+      saved += (float)(held - 1) * keys;
+    }
+    if (saved * H * (a.g.k_row + a.g.v_row) < SHARE_MIN_BYTES)
+      for (int g = 0; g < ng; ++g) gpfx[g] = 0;
+    n_groups_s = ng;
   }
   __syncthreads();
   const int ng = n_groups_s;
@@ -161,76 +184,57 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     const int t0 = tiles + scan_step(nt, part, tsum), c0 = chunks + scan_step(nc, part, csum);
     if (i < n) {
       first[i] = t0;
-      AttendSeq s;
-      s.tok0 = __ldcg(a.b.cu_q + i);
-      s.ntok = ntok[i];
-      s.slot = ntok[i] ? __ldcg(a.b.slots + i) : -1;
-      s.len = len[i];
-      s.pfx = pfx;
-      s.tile0 = t0;
-      s.chunk0 = c0;
-      s.group = grp[i];
-      a.w.seqs[i] = s;
-      for (int t = 0; t < ntok[i]; ++t) a.w.tok_seq[s.tok0 + t] = make_int2(i, grp[i]);
+      com[i] = c0;
+      a.w.seqs[i] = {tok0[i], ntok[i], slot[i], len[i], pfx, t0, c0, grp[i]};
+      for (int t = 0; t < ntok[i]; ++t) a.w.tok_seq[tok0[i] + t] = make_int2(i, grp[i]);
     }
     tiles += tsum;
     chunks += csum;
   }
   // groups: their cost, from it what a CTA has of it and the stripes, then the chunks of stripes
-  int32_t* gtok = ntok;                    // a group's tokens (the entries' are not needed any more)
   int cost = 0, wchunks = 0;
-  __syncthreads();
   for (int i0 = 0; i0 < ng; i0 += PLAN_THREADS) {
     const int i = i0 + tid;
-    int c = 0, tokens = 0;
+    int c = 0;
     if (i < ng) {
       const int at = gat[i];
       int last = i + 1 < ng ? gat[i + 1] : n;
       while (last > at + 1 && grp[last - 1] != i) --last;         // padding behind the group
-      tokens = a.w.seqs[last - 1].tok0 + a.w.seqs[last - 1].ntok - a.w.seqs[at].tok0;
-      const WideShape w(tokens, gpfx[i], G, 1);
+      gtok[i] = tok0[last - 1] + ntok[last - 1] - tok0[at];
+      const WideShape w(gtok[i], gpfx[i], G, 1);
       c = w.tiles * w.sum;
-      if (gpfx[i] && tokens * G > WIDE_ROWS / 2) any_full = 1;
+      if (gpfx[i] && gtok[i] * G > WIDE_ROWS / 2) any_full = 1;
     }
     int csum;
     const int c0 = cost + scan_step(c, part, csum);
-    if (i < ng) {
-      gcost[i] = c0;
-      gtok[i] = tokens;                                           // (i <= every entry of groups still to come)
-    }
+    if (i < ng) gcost[i] = c0;
     cost += csum;
-  }
-  __syncthreads();
-  const int H = a.g.n_kv_heads;
-  // (a stretch has to hold the beginning of a tile, whose cost is 2 in chunks of more than 128 rows)
-  const int wide_each = max(any_full ? 2 : 1, (H * cost + a.wide_grid - 1) / a.wide_grid);
-  const int stripe = (wide_each + 1) / 2;
-  for (int i0 = 0; i0 < ng; i0 += PLAN_THREADS) {
-    const int i = i0 + tid;
-    int nc = 0;
-    if (i < ng && gpfx[i]) {
-      const WideShape w(gtok[i], gpfx[i], G, stripe);
-      nc = w.chunks * w.stripes;
-    }
-    int nsum;
-    const int n0 = wchunks + scan_step(nc, part, nsum);
-    if (i < ng) {
-      AttendGroup r;
-      r.tok0 = a.w.seqs[gat[i]].tok0;
-      r.ntok = gtok[i];
-      r.slot = a.w.seqs[gat[i]].slot;
-      r.pfx = gpfx[i];
-      r.cost0 = gcost[i];
-      r.chunk0 = n0;
-      r.stripe = stripe;
-      r.pad0 = 0;
-      a.w.groups[i] = r;
-    }
-    wchunks += nsum;
   }
   if (tid == 0) { first[n] = tiles; gcost[ng] = cost; }
   __syncthreads();
   const int narrow_each = max(1, (H * tiles + a.narrow_grid - 1) / a.narrow_grid);
+  // (a stretch has to hold the beginning of a tile, whose cost is 2 in chunks of more than 128 rows)
+  const int wide_each = max(any_full ? 2 : 1, (H * cost + a.wide_grid - 1) / a.wide_grid);
+  const int stripe = (wide_each + 1) / 2;
+  auto group_of = [&](int i) { return AttendGroup{tok0[gat[i]], gtok[i], slot[gat[i]], gpfx[i], gcost[i], gchunk[i], stripe, 0}; };
+  if (cost) {
+    for (int i0 = 0; i0 < ng; i0 += PLAN_THREADS) {
+      const int i = i0 + tid;
+      int nc = 0;
+      if (i < ng && gpfx[i]) {
+        const WideShape w(gtok[i], gpfx[i], G, stripe);
+        nc = w.chunks * w.stripes;
+      }
+      int nsum;
+      const int n0 = wchunks + scan_step(nc, part, nsum);
+      if (i < ng) {
+        gchunk[i] = n0;
+        a.w.groups[i] = group_of(i);
+      }
+      wchunks += nsum;
+    }
+  }
+  __syncthreads();
   for (int k = tid; k < a.narrow_grid; k += PLAN_THREADS) {
     AttendStart s = {};
     s.h = -1;
@@ -238,17 +242,17 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     const int64_t u = (int64_t)k * narrow_each;
     if (u < H * tiles) {
       s.h = (int)u / tiles;
-      const int r = (int)u % tiles;
+      const int r = (int)u - s.h * tiles;
       int lo = 0, hi = n;                                       // last entry with first <= r that has tiles
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (first[mid] <= r) lo = mid; else hi = mid;
       }
       s.item = lo;
-      const int nt = max(1, (len[lo] - gpfx[grp[lo]] + NARROW_KEYS - 1) / NARROW_KEYS);
+      const int pfx = gpfx[grp[lo]], nt = max(1, (len[lo] - pfx + NARROW_KEYS - 1) / NARROW_KEYS);
       s.chunk = (r - first[lo]) / nt;
-      s.tile = (r - first[lo]) % nt;
-      s.seq = a.w.seqs[lo];
+      s.tile = r - first[lo] - s.chunk * nt;
+      s.seq = {tok0[lo], ntok[lo], slot[lo], len[lo], pfx, first[lo], com[lo], grp[lo]};
     }
     a.w.narrow_start[k] = s;
   }
@@ -259,42 +263,26 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     const int64_t u = (int64_t)k * wide_each;
     if (u < H * cost) {
       s.h = (int)u / cost;
-      const int r = (int)u % cost;
+      const int r = (int)u - s.h * cost;
       int lo = 0, hi = ng;
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
         if (gcost[mid] <= r) lo = mid; else hi = mid;
       }
       s.item = lo;
-      s.group = a.w.groups[lo];
+      s.group = group_of(lo);
       const WideShape w(s.group.ntok, s.group.pfx, G, stripe);
       const int x = r - gcost[lo];
       s.more = x / (w.stripe * w.sum);
       const int y = x - s.more * w.stripe * w.sum, nt = w.tiles_of(s.more);
-      s.chunk = min(y / (nt * 2), w.whole);                       // full chunks first; the last one may cost less
-      if (s.chunk == w.chunks) s.chunk = w.chunks - 1;
+      s.chunk = min(min(y / (nt * 2), w.whole), w.chunks - 1);    // full chunks first; the last one may cost less
       const int z = y - s.chunk * nt * 2, wl = w.weight(s.chunk, G);
       s.tile = s.more * w.stripe + (z + wl - 1) / wl;             // the first tile that begins in the stretch; may be the chunk's end
     }
     a.w.wide_start[k] = s;
   }
-  __syncthreads();
-  if (tid == 0) {
-    AttendHead h;
-    h.mark = ATTEND_MARK;
-    h.n_seqs = n;
-    h.n_tokens = a.b.n_tokens;
-    h.n_q_heads = a.n_q_heads;
-    h.n_kv_heads = H;
-    h.n_groups = ng;
-    h.narrow_tiles = tiles;
-    h.narrow_chunks = chunks;
-    h.narrow_each = narrow_each;
-    h.wide_cost = cost;
-    h.wide_chunks = wchunks;
-    h.wide_each = wide_each;
-    *a.w.head = h;
-  }
+  if (tid == 0)
+    *a.w.head = {ATTEND_MARK, n, a.b.n_tokens, a.n_q_heads, H, ng, tiles, chunks, narrow_each, cost, wchunks, wide_each};
 }
 
 // Rows whose keys were split: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m the largest m_i, and the same for lse.
@@ -490,13 +478,13 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   a.w = ptrs_of(l, workspace);
   a.G = n_q_heads / p->n_kv_heads;
   a.n_q_heads = n_q_heads;
-  a.share = share && b->n_seqs > 1;
+  a.share = !(share && b->n_seqs > 1) ? 0 : (int64_t)b->n_seqs * p->max_pages > SAME_INSIDE ? 1 : 2;
   a.narrow_grid = l.narrow_grid;
   a.wide_grid = l.wide_grid;
-  const size_t smem = sizeof(int32_t) * (7 * (size_t)b->n_seqs + 2);
+  const size_t smem = sizeof(int32_t) * (12 * (size_t)b->n_seqs + 2);
   if (smem > 48 * 1024)
-    ASL_CUDA(cudaFuncSetAttribute(attend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (7 * ATTEND_MAX_SEQS + 2)));
-  if (a.share) {
+    ASL_CUDA(cudaFuncSetAttribute(attend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (12 * ATTEND_MAX_SEQS + 2)));
+  if (a.share == 1) {
     launch_after(attend_same_kernel, dim3(b->n_seqs), dim3(SAME_THREADS), st, a.g, a.b, a.w.same);
     c->launches += 1;
   }

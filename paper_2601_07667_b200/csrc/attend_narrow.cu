@@ -136,11 +136,11 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           if (pg < end && lane == 0) {
             // (a page number out of range copies zeros or other rows of the pool, never from outside it)
             const int r = ((id * n_kv + w.h) << a.g.page_shift) + (key & ((1 << a.g.page_shift) - 1));
-            const uint32_t kd = base + st * S::STAGE + x * piece * 128, vd = base + st * S::STAGE + S::K_BYTES + x * piece * 128;
-            tma_load_2d(kd, &tm_k, full(st), 0, r);
-            if (!FP8) tma_load_2d(kd + NARROW_KEYS * 128, &tm_k, full(st), 64, r);
-            tma_load_2d(vd, &tm_v, full(st), 0, r);
-            tma_load_2d(vd + NARROW_KEYS * 128, &tm_v, full(st), 64, r);
+            // both 64-channel halves of a piece by one copy, one behind the other
+            const uint32_t kd = base + st * S::STAGE, vd = kd + S::K_BYTES + x * piece * 256;
+            if (FP8) tma_load_2d(kd + x * piece * 128, &tm_k, full(st), 0, r);
+            else tma_load_3d(kd + x * piece * 256, &tm_k, full(st), 0, r, 0);
+            tma_load_3d(vd, &tm_v, full(st), 0, r, 0);
           }
         }
       }
@@ -152,6 +152,10 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   } else if (any) {
     // ---- arithmetic ----
     const int gid = lane >> 2, tig = lane & 3, G = a.group_heads;
+    // where the rows that a lane loads lie in a stage: piece after piece, a piece's first halves before its second ones
+    const int krow = warp * 16 + (lane >> 4) * 8 + (lane & 7), vrow = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
+    const int piece = min(1 << a.g.page_shift, NARROW_KEYS), half_bytes = piece * 128;
+    const int k_at = (krow / piece * piece + krow) * 128, v_at = (vrow / piece * piece + vrow) * 128;
     int n = 0;
     bool more = true;
     while (more) {
@@ -209,12 +213,12 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
               mma16(x[1], qf[ks + 1], e4m3_pair(b[3]), e4m3_pair(b[3] >> 16));
             }
           } else {
-            const int row = warp * 16 + (lane >> 4) * 8 + (lane & 7);
+            const int row = krow;
 #pragma unroll
             for (int ks = 0; ks < 8; ++ks) {
               uint32_t b[4];
               const int ch = 2 * ks + ((lane >> 3) & 1);                      // 16-byte piece of the row
-              ldsm4(ks_ + (ch >> 3) * (NARROW_KEYS * 128) + row * 128 + (((ch & 7) ^ (row & 7)) << 4), b);
+              ldsm4(ks_ + k_at + (ch >> 3) * half_bytes + (((ch & 7) ^ (row & 7)) << 4), b);
               mma16(x[0], qf[ks], b[0], b[1]);
               mma16(x[1], qf[ks], b[2], b[3]);
             }
@@ -255,13 +259,12 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
               }
           // P rounded to bf16 for the tensor core (half a step, 2^-9 of a weight); l keeps the weights unrounded
           uint32_t pf[4] = {pack2(p[0][0], p[0][1]), pack2(p[0][2], p[0][3]), pack2(p[1][0], p[1][1]), pack2(p[1][2], p[1][3])};
-          const int vrow = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
           if (!careful) {
 #pragma unroll
             for (int jb = 0; jb < 8; ++jb) {
               uint32_t b[4];
               const int ch = 2 * jb + (lane >> 4);
-              ldsm4_t(vs_ + (ch >> 3) * (NARROW_KEYS * 128) + vrow * 128 + (((ch & 7) ^ (vrow & 7)) << 4), b);
+              ldsm4_t(vs_ + v_at + (ch >> 3) * half_bytes + (((ch & 7) ^ (vrow & 7)) << 4), b);
               mma16(o[2 * jb], pf, b[0], b[1]);
               mma16(o[2 * jb + 1], pf, b[2], b[3]);
             }
@@ -278,7 +281,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
               for (int jb = 0; jb < 8; ++jb) {
                 uint32_t b[4];
                 const int ch = 2 * jb + (lane >> 4);
-                ldsm4_t(vs_ + (ch >> 3) * (NARROW_KEYS * 128) + vrow * 128 + (((ch & 7) ^ (vrow & 7)) << 4), b);
+                ldsm4_t(vs_ + v_at + (ch >> 3) * half_bytes + (((ch & 7) ^ (vrow & 7)) << 4), b);
                 float d0[4] = {0, 0, 0, 0}, d1[4] = {0, 0, 0, 0};
                 mma16(d0, pf, b[0] & keep[0], b[1] & keep[1]);
                 mma16(d1, pf, b[2] & keep[0], b[3] & keep[1]);
@@ -368,11 +371,13 @@ asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, const Attend
   const cuuint64_t n_rows = (cuuint64_t)p->n_pages * p->n_kv_heads * p->page_size;
   const cuuint32_t piece = p->page_size < NARROW_KEYS ? p->page_size : NARROW_KEYS;
   CUtensorMap tm_k, tm_v;
-  const cuuint64_t dims[2] = {128, n_rows};
-  const cuuint64_t ks[1] = {(cuuint64_t)a.g.k_row}, vs[1] = {(cuuint64_t)a.g.v_row};
-  const cuuint32_t kbox[2] = {fp8 ? 128u : 64u, piece}, vbox[2] = {64, piece};
-  if (!asl_make_map(&tm_k, fp8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.g.k, 2, dims, ks, kbox)) return ASL_ERR_CUDA;
-  if (!asl_make_map(&tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.g.v, 2, dims, vs, vbox)) return ASL_ERR_CUDA;
+  // E4M3 rows are 128 bytes; bf16 rows two halves of that, the outermost dimension
+  const cuuint64_t dims8[2] = {128, n_rows}, stride8[1] = {128};
+  const cuuint64_t dims[3] = {64, n_rows, 2}, strides[2] = {256, 128};
+  const cuuint32_t box8[2] = {128, piece}, box[3] = {64, piece, 2};
+  const bool k_map = fp8 ? asl_make_map(&tm_k, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.g.k, 2, dims8, stride8, box8)
+                         : asl_make_map(&tm_k, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.g.k, 3, dims, strides, box);
+  if (!k_map || !asl_make_map(&tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.g.v, 3, dims, strides, box)) return ASL_ERR_CUDA;
   auto kernel = fp8 ? attend_narrow_kernel<true> : attend_narrow_kernel<false>;
   const int smem = fp8 ? NarrowSmem<true>::BYTES : NarrowSmem<false>::BYTES;
   ASL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));

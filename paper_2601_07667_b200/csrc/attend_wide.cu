@@ -32,7 +32,7 @@ struct WideSmem {
   static constexpr int BYTES = MISC + 16 + 1024;
   static constexpr int THREADS = FP8 ? 512 : 384;
   // Registers a thread: a row of 128 logits stays in them.  Launched with REGS each; the warpgroups' shares are no more together.
-  static constexpr int REGS = FP8 ? 128 : 168, REGS_FEW = FP8 ? 64 : 72, REGS_ROWS = FP8 ? 192 : 216;
+  static constexpr int REGS = FP8 ? 128 : 168, REGS_FEW = FP8 ? 40 : 72, REGS_ROWS = 216;
   static_assert(REGS * THREADS >= REGS_FEW * (THREADS - 256) + REGS_ROWS * 256, "a warpgroup would wait for registers");
   static_assert(N_BARS * 8 <= 256 && BYTES <= 232448, "shared memory budget of one CTA");
 };
@@ -125,14 +125,14 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   auto bar = [&](int i) { return base + S::BARS + 8 * i; };
   if (threadIdx.x == 0) {
     // (tiles and queries are given back by both issuing warps)
-    for (int i = 0; i < K_RING; ++i) { mbar_init(bar(S::KF + i), FP8 ? 128 : 1); mbar_init(bar(S::KE + i), 2); }
+    for (int i = 0; i < K_RING; ++i) { mbar_init(bar(S::KF + i), FP8 ? 4 : 1); mbar_init(bar(S::KE + i), 2); }
     for (int i = 0; i < S::V_RING; ++i) { mbar_init(bar(S::VF + i), 1); mbar_init(bar(S::VE + i), 2); }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bar(S::SF + i), 1);
       mbar_init(bar(S::PF + i), 4);
       mbar_init(bar(S::OD + i), 1);
       mbar_init(bar(S::CF + i), 1);
-      mbar_init(bar(S::CE + i), 128);
+      mbar_init(bar(S::CE + i), 4);
     }
     mbar_init(bar(S::QF), 1);
     mbar_init(bar(S::QE), 2);
@@ -441,8 +441,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
                 make_uint4(e4m3_pair(v.z), e4m3_pair(v.z >> 16), e4m3_pair(v.w), e4m3_pair(v.w >> 16));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-          mbar_arrive(bar(S::KF + ks));
-          mbar_arrive(bar(S::CE + cs));
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(bar(S::KF + ks));
+            mbar_arrive(bar(S::CE + cs));
+          }
         }
         if (ok) more = w.next(a);
       }
