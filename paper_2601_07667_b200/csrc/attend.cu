@@ -144,13 +144,19 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     __syncthreads();
   }
   // Groups: an entry joins the group before it where that group then saves no less than without it.
+  int32_t* own = gtok;                     // tokens that all of an entry's see
+  for (int i = tid; i < n; i += PLAN_THREADS) {
+    own[i] = max(0, len[i] - ntok[i]) >> a.g.page_shift << a.g.page_shift;
+    com[i] = min(own[i], com[i]);
+  }
+  __syncthreads();
   if (tid == 0) {
     int ng = 0, held = 0, keys = 0;                          // of the open group: entries (0: none is open), shared tokens
     float saved = 0.0f;                                      // keys read less often, by all groups so far
-#pragma unroll 4
+    int has = ntok[0], mine = own[0], with = com[0];
     for (int i = 0; i < n; ++i) {
-      const int has = ntok[i], own = max(0, len[i] - has) >> a.g.page_shift << a.g.page_shift;     // all its tokens see these
-      const int both = min(keys, min(own, com[i]));
+      const int j = min(i + 1, n - 1), has2 = ntok[j], mine2 = own[j], with2 = com[j];       // (ahead of this entry's stores)
+      const int both = min(keys, with);
       const bool joins = has && held && both > 0 && (float)held * both >= (float)(held - 1) * keys;
       if (!joins && held) {
         gpfx[ng - 1] = held > 1 ? keys : 0;
@@ -158,8 +164,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       }
       if (!joins && has) gat[ng++] = i;
       held = has ? (joins ? held + 1 : 1) : 0;
-      keys = joins ? both : own;
+      keys = joins ? both : mine;
       grp[i] = has ? ng - 1 : -1;
+      has = has2; mine = mine2; with = with2;
     }
     if (held) {
       gpfx[ng - 1] = held > 1 ? keys : 0;

@@ -126,14 +126,13 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           ids = first + lane < end ? __ldcg(row + first + lane) : -1;
         }
         if (n >= STAGES && !mbar_wait(empty(st), (n / STAGES - 1) & 1, s_abort, 201, true)) { more = false; break; }
-        int count = 0;
-        for (int x = 0; x < per; ++x) count += ((key0 + x * piece) >> a.g.page_shift) < end;
-        if (lane == 0) mbar_expect_tx(full(st), (uint32_t)(count * piece * (a.g.k_row + a.g.v_row)));
+        const int count = min(per, max(0, ((end << a.g.page_shift) - key0 + piece - 1) / piece));       // pieces of pages that it has
+        if (elect_one()) mbar_expect_tx(full(st), (uint32_t)(count * piece * (a.g.k_row + a.g.v_row)));
         __syncwarp();
         for (int x = 0; x < per; ++x) {
           const int key = key0 + x * piece, pg = key >> a.g.page_shift;
           const int id = __shfl_sync(0xffffffffu, ids, (pg - first) & 31);
-          if (pg < end && lane == 0) {
+          if (pg < end && elect_one()) {
             // (a page number out of range copies zeros or other rows of the pool, never from outside it)
             const int r = ((id * n_kv + w.h) << a.g.page_shift) + (key & ((1 << a.g.page_shift) - 1));
             // both 64-channel halves of a piece by one copy, one behind the other

@@ -300,12 +300,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           const uint32_t kd = base + (FP8 ? S::CODES + (n & 1) * TILE_HALF : S::K + ks * TILE_BYTES);
           const uint32_t kpar = ((FP8 ? n >> 1 : n / K_RING) & 1) ^ 1;
           if (!mbar_wait(kfree, kpar, s_abort, 212, true)) { ok = false; break; }
-          if (lane == 0) mbar_expect_tx(kbar, (uint32_t)(np * page * a.g.k_row));
+          const int r0 = (ids * a.g.n_kv_heads + w.h) << shift;
+          if (elect_one()) mbar_expect_tx(kbar, (uint32_t)(np * page * a.g.k_row));
           __syncwarp();
           for (int x = 0; x < np; ++x) {
-            const int id = __shfl_sync(0xffffffffu, ids, t * per + x - first);
-            const int r = (id * a.g.n_kv_heads + w.h) << shift;
-            if (lane == 0) {
+            const int r = __shfl_sync(0xffffffffu, r0, t * per + x - first);
+            if (elect_one()) {
               tma_load_2d(kd + x * page * 128, &tm_k, kbar, 0, r);
               if (!FP8) tma_load_2d(kd + TILE_HALF + x * page * 128, &tm_k, kbar, 64, r);
             }
@@ -315,12 +315,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             ++n;                             // K of this tile is in flight
             break;
           }
-          if (lane == 0) mbar_expect_tx(bar(S::VF + vs), (uint32_t)(np * page * 256));
+          if (elect_one()) mbar_expect_tx(bar(S::VF + vs), (uint32_t)(np * page * 256));
           __syncwarp();
           for (int x = 0; x < np; ++x) {
-            const int id = __shfl_sync(0xffffffffu, ids, t * per + x - first);
-            const int r = (id * a.g.n_kv_heads + w.h) << shift;
-            if (lane == 0) {
+            const int r = __shfl_sync(0xffffffffu, r0, t * per + x - first);
+            if (elect_one()) {
               const uint32_t vd = base + S::V + vs * TILE_BYTES + x * page * 128;
               tma_load_2d(vd, &tm_v, bar(S::VF + vs), 0, r);
               tma_load_2d(vd + TILE_HALF, &tm_v, bar(S::VF + vs), 64, r);
