@@ -27,7 +27,7 @@ struct WideSmem {
   static constexpr int CODES = V + V_RING * TILE_BYTES;             // E4M3 tiles as they come
   static constexpr int BARS = CODES + (FP8 ? 2 * TILE_HALF : 0);
   static constexpr int KF = 0, KE = KF + K_RING, VF = KE + K_RING, VE = VF + 3, SF = VE + 3, PF = SF + 2, OD = PF + 2, QF = OD + 2,
-                       QE = QF + 1, CF = QE + 1, CE = CF + 2, DRAIN = CE + 2, N_BARS = DRAIN + 2;
+                       QE = QF + 1, CF = QE + 1, CE = CF + 2, DRAIN = CE + 2, TURN = DRAIN + 2, N_BARS = TURN + 2;
   static constexpr int MISC = BARS + 256;
   static constexpr int BYTES = MISC + 16 + 1024;
   static constexpr int THREADS = FP8 ? 512 : 384;
@@ -138,6 +138,8 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     mbar_init(bar(S::QE), 2);
     mbar_init(bar(S::DRAIN), 1);
     mbar_init(bar(S::DRAIN + 1), 1);
+    mbar_init(bar(S::TURN), 1);
+    mbar_init(bar(S::TURN + 1), 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -346,7 +348,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0) + s * 128;
       const uint32_t id_full = instr_desc(128, WIDE_KEYS), id_pv = instr_desc(128, 128) | B_MN_MAJOR;
       int n = 0;                           // tiles before this run
-      uint32_t pv = 0;                     // parity of the next product P V
+      uint32_t pv = 0, turns = 0;          // parity of the next product P V; batches given in turn
       bool ok = true, more = true;
       for (int run = 0; ok && more; ++run) {
         const bool full = __shfl_sync(0xffffffffu, (int)w.full(), 0);
@@ -358,6 +360,16 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         };
         auto values_here = [&](int j) {
           if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar(S::VF + (n + j) % S::V_RING), ((n + j) / S::V_RING) & 1, s_abort, 224, true));
+        };
+        // Streams of full chunks give their batches in turn: interleaved, two batches would both end when the later does, and
+        // the streams would do everything else at the same time too.
+        auto take_turn = [&]() {
+          if (full && ok && (s == 1 || turns > 0))
+            ok = __all_sync(0xffffffffu, mbar_wait(bar(S::TURN + s), (s == 1 ? turns : turns - 1) & 1, s_abort, 227, true));
+        };
+        auto give_turn = [&]() {
+          if (full && lane == 0) mbar_arrive(bar(S::TURN + (s ^ 1)));
+          if (full) ++turns;
         };
         auto scores = [&](int j) {         // S of tile j
           const int ks = (n + j) % K_RING, left = pfx - j * WIDE_KEYS;
@@ -376,9 +388,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         };
         ok = __all_sync(0xffffffffu, mbar_wait(bar(S::QF), run & 1, s_abort, 222, true));
         keys_here(first);
+        take_turn();
         if (ok && first < nt) {
           tc_fence_after();
           scores(first);
+          give_turn();
         } else if (ok && lane == 0) {
           mbar_arrive(bar(S::QE));         // a run of one tile: the other stream's
         }
@@ -387,6 +401,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           values_here(j);                  // (tiles are waited for before the weights, while the pipe still has products)
           keys_here(j + step);
           ok = ok && __all_sync(0xffffffffu, mbar_wait(bar(S::PF + s), pv, s_abort, 223, true));
+          take_turn();
           if (!ok) break;
           tc_fence_after();
           const uint64_t vd = smem_desc_mn(base + S::V + vs * TILE_BYTES, TILE_HALF);
@@ -405,6 +420,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           __syncwarp();
           pv ^= 1u;
           if (j + step < nt) scores(j + step);
+          give_turn();
         }
         n += nt;
         if (ok) more = w.next(a);
