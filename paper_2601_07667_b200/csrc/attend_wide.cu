@@ -87,9 +87,9 @@ struct Walk {
   __device__ __forceinline__ int64_t slot() const { return (int64_t)h * chunks + g.chunk0 + stripe * n_chunks + chunk + blockIdx.x; }
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {        // NaN where one is
+__device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 __device__ __forceinline__ float row_max(const uint32_t (&x)[4][32]) {
@@ -103,10 +103,6 @@ __device__ __forceinline__ float row_max(const uint32_t (&x)[4][32]) {
   }
   return max3(max3(m[0], m[1], m[2]), m[3], m[3]);
 }
-// Which column pairs of 32 take the polynomial: see pair_is_poly of the scorer for what it is.
-constexpr int POLY_OF_32 = 8;
-__device__ __forceinline__ constexpr bool poly_pair(int i) { return ((i & 31) * POLY_OF_32) % 32 + POLY_OF_32 >= 32; }
-
 template <int N>
 __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
@@ -188,14 +184,13 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int k = 0; k < WIDE_KEYS; ++k)
               if (k >= nk) x[k >> 5][k & 31] = 0xff800000u;         // -inf
           }
-          // the row's largest logit; NaN stays NaN
-          float mx = row_max(x) * c;
-          if (mx == INFINITY) mx = __int_as_float(0x7fffffff);      // infinite logits: the row is NaN, as in inf - inf
+          // the row's largest logit (a NaN, or infinity less itself, makes weights NaN below, and with them the row)
+          const float mx = row_max(x) * c;
           const bool first = t == t0;
           if (first) {
             m = mx;
           } else {
-            const bool grow = !(mx <= m + RESCALE);                 // NaN too
+            const bool grow = mx > m + RESCALE;
             if (__any_sync(0xffffffffu, grow)) {
               if (!__all_sync(0xffffffffu, mbar_wait(bar(S::OD + s), (it - 1) & 1, s_abort, 232, true))) { ok = false; break; }
               tc_fence_after();
@@ -225,7 +220,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
             for (int e = 0; e < 32; ++e) {
               const int col = 64 * k + 2 * e;
               const f32x2 z = fma2(pku(x[col >> 5][col & 31], x[col >> 5][(col & 31) + 1]), c2, m2);
-              const f32x2 y = poly_pair(e) ? ex2_pair_poly<false>(z) : ex2_pair_mufu(z);
+              const f32x2 y = ex2_pair_mufu(z);
               if (e & 1) l3 = add2(l3, y); else l2 = add2(l2, y);
               float lo, hi;
               upk(y, lo, hi);
@@ -367,10 +362,6 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           if (full && ok && (s == 1 || turns > 0))
             ok = __all_sync(0xffffffffu, mbar_wait(bar(S::TURN + s), (s == 1 ? turns : turns - 1) & 1, s_abort, 227, true));
         };
-        auto give_turn = [&]() {
-          if (full && lane == 0) mbar_arrive(bar(S::TURN + (s ^ 1)));
-          if (full) ++turns;
-        };
         auto scores = [&](int j) {         // S of tile j
           const int ks = (n + j) % K_RING, left = pfx - j * WIDE_KEYS;
           const uint64_t qd = smem_desc(base + (full ? s : 0) * 128 * 128), kd = smem_desc(base + S::K + ks * TILE_BYTES);
@@ -379,6 +370,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
 #pragma unroll
             for (int x = 0; x < 8; ++x)
               tc_mma(tm, qd + ((x >> 2) * (S::Q_HALF >> 4) + (x & 3) * 2), kd + ((x >> 2) * (TILE_HALF >> 4) + (x & 3) * 2), id, x > 0);
+            if (full) mbar_arrive(bar(S::TURN + (s ^ 1)));          // the other stream's turn
             tc_commit(bar(S::SF + s));
             tc_commit(bar(S::KE + ks));
             if (!full) tc_commit(bar(S::KE + ks));                  // nobody else reads it
@@ -392,7 +384,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         if (ok && first < nt) {
           tc_fence_after();
           scores(first);
-          give_turn();
+          turns += full;
         } else if (ok && lane == 0) {
           mbar_arrive(bar(S::QE));         // a run of one tile: the other stream's
         }
@@ -420,7 +412,8 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
           __syncwarp();
           pv ^= 1u;
           if (j + step < nt) scores(j + step);
-          give_turn();
+          else if (full && lane == 0) mbar_arrive(bar(S::TURN + (s ^ 1)));
+          turns += full;
         }
         n += nt;
         if (ok) more = w.next(a);
