@@ -227,10 +227,10 @@ __global__ void __launch_bounds__(128) pages_trim_kernel(PagePool g, const int32
 }
 
 // Where row `pos` of a slot lies, in rows of its kv head's pool; -1 where it may not be written.
-__device__ __forceinline__ int64_t place_of(const PagePool& g, int slot, int pos, int h, bool& wrong) {
+__device__ __forceinline__ int place_of(const PagePool& g, int slot, int pos, int h, bool& wrong) {
   const int id = __ldcg(g.table + (int64_t)slot * g.max_pages + (pos >> g.page_shift));
   if ((unsigned)id >= (unsigned)g.n_pages || __ldcg(g.refs + id) != 1) { wrong = true; return -1; }
-  return (((int64_t)id * g.n_kv_heads + h) << g.page_shift) + (pos & ((1 << g.page_shift) - 1));
+  return ((id * g.n_kv_heads + h) << g.page_shift) + (pos & ((1 << g.page_shift) - 1));
 }
 
 struct RowSource {
@@ -244,15 +244,16 @@ struct RowSource {
   const int32_t* off;
 };
 
-constexpr int ROWS = 4;                    // rows per thread, 16 threads a row
-constexpr int BLOCK_ROWS = 16 * ROWS;
-
-// Kept rows into pages.  As compact_kv_kernel: 16 threads move a row's 16-byte vectors, four rows' K and V in flight.
-template <bool CACHED>
+// Kept rows into pages.  A block takes R rows of one kv head: first a thread a row finds where it comes from and goes to (three
+// dependent loads: list, table, count or table), then 16 threads move a row's 16-byte vectors, four rows' K and V in flight each
+// (as compact_kv_kernel).  Found by all 16 threads of a row and 64 rows a block, half of four 24K-token prompts (268 MB
+// moved) took 57 us.
+template <bool CACHED, int R>
 __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSource x, const int32_t* __restrict__ idx,
                                                             const int32_t* __restrict__ dst, int64_t sum_kept) {
+  __shared__ int from_s[R], to_s[R];
   pdl_wait_predecessor();
-  const int b = blockIdx.z, h = blockIdx.y;
+  const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
   const int slot = __ldcg(dst + b);
   int kept, src = 0, n_src;
   int64_t at, tok_off = 0;
@@ -269,56 +270,68 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
     const AslReq rq = x.req[b];
     kept = rq.kept; at = rq.kept_off; n_src = rq.n; tok_off = rq.tok_off;
   }
-  if (blockIdx.x * BLOCK_ROWS >= kept) return;
+  const int r0 = blockIdx.x * R;
+  if (r0 >= kept) return;
   if ((unsigned)slot >= (unsigned)g.max_seqs) {
-    if (threadIdx.x == 0) note_error(g.err, ASL_ERR_INVALID, slot);
+    if (tid == 0) note_error(g.err, ASL_ERR_INVALID, slot);
     return;
   }
-  const int n_dst = min(__ldcg(g.len + slot), g.max_pages << g.page_shift);
-  const int c = threadIdx.x % 16, r0 = blockIdx.x * BLOCK_ROWS + threadIdx.x / 16;
-  const int k_vec = g.k_row / 16, v_vec = g.v_row / 16;
-  const int32_t* list = idx + (int64_t)h * sum_kept + at;
-  bool wrong = false;
-  int64_t to[ROWS];
-  const uint8_t *kr[ROWS], *vr[ROWS];
-  int tok[ROWS];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    const int r = r0 + 16 * i;
-    tok[i] = -1;
-    to[i] = -1;
+  if (tid < R) {
+    const int r = r0 + tid;
+    int from = -1, to = -1;
     if (r < kept) {
-      tok[i] = __ldcg(list + r);
-      if (r >= n_dst || (unsigned)tok[i] >= (unsigned)n_src) wrong = true;
-      else to[i] = place_of(g, slot, r, h, wrong);
+      bool wrong = false;
+      const int tok = __ldcg(idx + (int64_t)h * sum_kept + at + r);
+      const int n_dst = min(__ldcg(g.len + slot), g.max_pages << g.page_shift);
+      if (r >= n_dst || (unsigned)tok >= (unsigned)n_src) {
+        wrong = true;
+      } else {
+        from = tok;
+        if (CACHED) {
+          const int id = __ldcg(g.table + (int64_t)src * g.max_pages + (tok >> g.page_shift));
+          if ((unsigned)id >= (unsigned)g.n_pages) wrong = true;
+          from = ((id * g.n_kv_heads + h) << g.page_shift) + (tok & ((1 << g.page_shift) - 1));
+        }
+        to = place_of(g, slot, r, h, wrong);
+        if (wrong) to = -1;
+      }
+      if (wrong) note_error(g.err, ASL_ERR_INVALID, slot);
+    }
+    from_s[tid] = from;
+    to_s[tid] = to;
+  }
+  __syncthreads();
+  const int c = tid % 16, k_vec = g.k_row / 16;
+  const uint8_t* ks = CACHED ? g.k : x.k + tok_off * x.ks_t + (int64_t)h * x.ks_h;
+  const uint8_t* vs = CACHED ? g.v : x.v + tok_off * x.vs_t + (int64_t)h * x.vs_h;
+  const int64_t ks_t = CACHED ? g.k_row : x.ks_t, vs_t = CACHED ? g.v_row : x.vs_t;
+#pragma unroll
+  for (int q0 = 0; q0 < R; q0 += 64) {
+    uint4 kv[4], vv[4];
+    int to[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = q0 + 16 * i + tid / 16, from = from_s[r];
+      to[i] = to_s[r];
+      if (to[i] >= 0 && c < k_vec) kv[i] = __ldcs(reinterpret_cast<const uint4*>(ks + from * ks_t) + c);
+      if (to[i] >= 0) vv[i] = __ldcs(reinterpret_cast<const uint4*>(vs + from * vs_t) + c);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (to[i] >= 0 && c < k_vec) __stcs(reinterpret_cast<uint4*>(g.k + (int64_t)to[i] * g.k_row) + c, kv[i]);
+      if (to[i] >= 0) __stcs(reinterpret_cast<uint4*>(g.v + (int64_t)to[i] * g.v_row) + c, vv[i]);
     }
   }
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    if (to[i] < 0) continue;
-    if (CACHED) {
-      const int id = __ldcg(g.table + (int64_t)src * g.max_pages + (tok[i] >> g.page_shift));
-      if ((unsigned)id >= (unsigned)g.n_pages) { wrong = true; to[i] = -1; continue; }
-      const int64_t from = (((int64_t)id * g.n_kv_heads + h) << g.page_shift) + (tok[i] & ((1 << g.page_shift) - 1));
-      kr[i] = g.k + from * g.k_row;
-      vr[i] = g.v + from * g.v_row;
-    } else {
-      kr[i] = x.k + (tok_off + tok[i]) * x.ks_t + (int64_t)h * x.ks_h;
-      vr[i] = x.v + (tok_off + tok[i]) * x.vs_t + (int64_t)h * x.vs_h;
-    }
-  }
-  uint4 kv[ROWS], vv[ROWS];
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    if (to[i] >= 0 && c < k_vec) kv[i] = __ldcs(reinterpret_cast<const uint4*>(kr[i]) + c);
-    if (to[i] >= 0 && c < v_vec) vv[i] = __ldcs(reinterpret_cast<const uint4*>(vr[i]) + c);
-  }
-#pragma unroll
-  for (int i = 0; i < ROWS; ++i) {
-    if (to[i] >= 0 && c < k_vec) __stcs(reinterpret_cast<uint4*>(g.k + to[i] * g.k_row) + c, kv[i]);
-    if (to[i] >= 0 && c < v_vec) __stcs(reinterpret_cast<uint4*>(g.v + to[i] * g.v_row) + c, vv[i]);
-  }
-  if (wrong) note_error(g.err, ASL_ERR_INVALID, slot);
+}
+
+// 256 rows a block where that still makes a few blocks for every SM, else 64.
+template <bool CACHED>
+void launch_rows(const asl_ctx* c, const PagePool& g, const RowSource& x, const int32_t* idx, const int32_t* dst, int64_t sum_kept,
+                 int max_kept, int jobs, cudaStream_t st) {
+  if ((int64_t)sum_kept * g.n_kv_heads >= (int64_t)c->sm_count * 4 * 256)
+    launch_after(rows_to_pages_kernel<CACHED, 256>, dim3((max_kept + 255) / 256, g.n_kv_heads, jobs), dim3(256), st, g, x, idx, dst, sum_kept);
+  else
+    launch_after(rows_to_pages_kernel<CACHED, 64>, dim3((max_kept + 63) / 64, g.n_kv_heads, jobs), dim3(256), st, g, x, idx, dst, sum_kept);
 }
 
 // A step's rows at the ends of their sequences: a block column per sequence, 16 threads a (token, kv head) row.
@@ -344,7 +357,7 @@ __global__ void __launch_bounds__(128) pages_append_kernel(PagePool g, asl_batch
     uint4 kv = make_uint4(0, 0, 0, 0);
     if (c * 16 < g.k_row) kv = __ldcg(reinterpret_cast<const uint4*>(kr) + c);
     const uint4 vv = __ldcg(reinterpret_cast<const uint4*>(vr) + c);
-    const int64_t to = wrong ? -1 : place_of(g, slot, pos, h, wrong);
+    const int64_t to = wrong ? -1 : (int64_t)place_of(g, slot, pos, h, wrong);
     if (to >= 0) {
       if (c * 16 < g.k_row) reinterpret_cast<uint4*>(g.k + to * g.k_row)[c] = kv;
       reinterpret_cast<uint4*>(g.v + to * g.v_row)[c] = vv;
@@ -448,8 +461,7 @@ asl_status asl_pages_store(asl_ctx* c, const asl_pages* p, int32_t layer, const 
   x.req = c->d_req;
   x.latch = c->latch_stat;
   x.cur_layer = c->cur_layer;
-  const dim3 grid((c->max_kept + BLOCK_ROWS - 1) / BLOCK_ROWS, q.n_kv_heads, q.batch);
-  launch_after(rows_to_pages_kernel<false>, grid, dim3(256), static_cast<cudaStream_t>(stream), page_pool(p, layer), x, idx, slots, c->sum_kept);
+  launch_rows<false>(c, page_pool(p, layer), x, idx, slots, c->sum_kept, c->max_kept, q.batch, static_cast<cudaStream_t>(stream));
   return launched(c, 1);
 }
 
@@ -463,8 +475,7 @@ asl_status asl_pages_compact(asl_ctx* c, const asl_pages* p, int32_t layer, cons
   RowSource x = {};
   x.src = src;
   x.off = off;
-  const dim3 grid((max_kept + BLOCK_ROWS - 1) / BLOCK_ROWS, p->n_kv_heads, n_jobs);
-  launch_after(rows_to_pages_kernel<true>, grid, dim3(256), static_cast<cudaStream_t>(stream), page_pool(p, layer), x, idx, dst, sum_kept);
+  launch_rows<true>(c, page_pool(p, layer), x, idx, dst, sum_kept, max_kept, n_jobs, static_cast<cudaStream_t>(stream));
   return launched(c, 1);
 }
 
