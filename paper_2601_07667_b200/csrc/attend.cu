@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   int32_t* first = sm + 10 * n;            // [n + 1] narrow tiles before
   int32_t* gcost = sm + 11 * n + 1;        // [n + 1] wide cost before
   if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; }
-  for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tok_seq[t] = make_int2(-1, -1);
+  for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tokens[t].seq.ntok = 0;
   __syncthreads();
   for (int i = tid; i < n; i += PLAN_THREADS) {
     const int s = __ldcg(a.b.slots + i), t0 = __ldcg(a.b.cu_q + i), t1 = __ldcg(a.b.cu_q + i + 1);
@@ -193,7 +193,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       first[i] = t0;
       com[i] = c0;
       a.w.seqs[i] = {tok0[i], ntok[i], slot[i], len[i], pfx, t0, c0, grp[i]};
-      for (int t = 0; t < ntok[i]; ++t) a.w.tok_seq[tok0[i] + t] = make_int2(i, grp[i]);
     }
     tiles += tsum;
     chunks += csum;
@@ -242,6 +241,14 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     }
   }
   __syncthreads();
+  for (int i = tid; i < n; i += PLAN_THREADS) {
+    if (!ntok[i]) continue;
+    const int pfx = gpfx[grp[i]];
+    AttendToken r = {};
+    r.seq = {tok0[i], ntok[i], slot[i], len[i], pfx, first[i], com[i], grp[i]};
+    if (pfx) r.group = group_of(grp[i]);
+    for (int t = 0; t < ntok[i]; ++t) a.w.tokens[tok0[i] + t] = r;
+  }
   for (int k = tid; k < a.narrow_grid; k += PLAN_THREADS) {
     AttendStart s = {};
     s.h = -1;
@@ -294,7 +301,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
 
 // Rows whose keys were split: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m the largest m_i, and the same for lse.
 // WARPS warps a row, four channels a lane, up to eight parts in flight each; parts in a fixed order, so that a row comes out the
-// same on every run.  A chain of four round trips (token, sequence and group, parts, result) bounds it where rows are few.
+// same on every run.  A chain of two round trips (token, parts) bounds it where rows are few.
 template <int WARPS>
 __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
   __shared__ float4 joined[4][32];
@@ -303,11 +310,10 @@ __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
   const int row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x;
   const bool exists = row < a.n_tokens * a.n_q_heads;
   const int t = exists ? row / a.n_q_heads : 0, head = row - t * a.n_q_heads, G = a.group_heads, h = head / G, g = head - h * G;
-  const int2 who = __ldcg(a.w.tok_seq + t);
+  const AttendSeq s = load_seq(&a.w.tokens[t].seq);
+  const AttendGroup gr = load_group(&a.w.tokens[t].group);
   const AttendHead hd = load_head(a.w.head);
-  if (!plan_fits(a, hd) || !exists || who.x < 0) return;              // (the same for all warps of a row)
-  const AttendSeq s = load_seq(a.w.seqs + who.x);
-  const AttendGroup gr = load_group(a.w.groups + who.y);
+  if (!plan_fits(a, hd) || !exists || s.ntok == 0) return;            // (the same for all warps of a row)
   const int nt = narrow_tiles_of(s), lr = (t - s.tok0) * G + g, chunk = lr / NARROW_ROWS;
   const int ta = h * hd.narrow_tiles + s.tile0 + chunk * nt;
   const int c0 = ta / hd.narrow_each, c1 = (ta + nt - 1) / hd.narrow_each;
@@ -423,7 +429,7 @@ AttendLayout layout_of(int sm_count, int n_kv_heads, int n_seqs, int n_tokens, i
   l.seqs = take(sizeof(AttendSeq) * n_seqs);
   l.groups = take(sizeof(AttendGroup) * n_seqs);
   l.same = take(sizeof(int32_t) * n_seqs);
-  l.tok_seq = take(sizeof(int2) * n_tokens);
+  l.tokens = take(sizeof(AttendToken) * n_tokens);
   l.narrow_start = take(sizeof(AttendStart) * l.narrow_grid);
   l.wide_start = take(sizeof(AttendStart) * l.wide_grid);
   l.wide_row0 = (int64_t)(NARROW_ROWS * narrow_slots);
@@ -440,7 +446,7 @@ AttendPtrs ptrs_of(const AttendLayout& l, void* workspace) {
   p.seqs = reinterpret_cast<AttendSeq*>(w + l.seqs);
   p.groups = reinterpret_cast<AttendGroup*>(w + l.groups);
   p.same = reinterpret_cast<int32_t*>(w + l.same);
-  p.tok_seq = reinterpret_cast<int2*>(w + l.tok_seq);
+  p.tokens = reinterpret_cast<AttendToken*>(w + l.tokens);
   p.narrow_start = reinterpret_cast<AttendStart*>(w + l.narrow_start);
   p.wide_start = reinterpret_cast<AttendStart*>(w + l.wide_start);
   p.ml = reinterpret_cast<float2*>(w + l.ml);

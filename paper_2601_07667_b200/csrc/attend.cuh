@@ -30,6 +30,8 @@ struct __align__(16) AttendGroup {
   int32_t tok0, ntok, slot, pfx;
   int32_t cost0, chunk0, stripe, pad0; // wide cost and chunks (of stripes) before; tiles of a stripe
 };
+// What the joining of a token's rows needs to know, in one round trip (seq.ntok 0: nobody's token).
+struct __align__(16) AttendToken { AttendSeq seq; AttendGroup group; };
 // Where a CTA's stretch begins (h < 0: it has none), with all that it needs to know there: one round trip to memory.
 struct __align__(16) AttendStart {
   int32_t h, item, chunk, tile;
@@ -38,7 +40,7 @@ struct __align__(16) AttendStart {
 };
 
 struct AttendLayout {      // byte offsets in the workspace
-  size_t head, seqs, groups, same, tok_seq, narrow_start, wide_start, ml, o, total;
+  size_t head, seqs, groups, same, tokens, narrow_start, wide_start, ml, o, total;
   int64_t wide_row0;
   int32_t narrow_grid, wide_grid;
 };
@@ -48,7 +50,7 @@ struct AttendPtrs {
   AttendSeq* seqs;
   AttendGroup* groups;
   int32_t* same;           // [n_seqs] leading pages that an entry has in common with the one before
-  int2* tok_seq;           // [n_tokens] a token's entry (-1: nobody's) and group
+  AttendToken* tokens;     // [n_tokens]
   AttendStart* narrow_start;
   AttendStart* wide_start;
   float2* ml;              // of every part's rows: 16 of a narrow slot, then, from wide_row0 on, 256 of a wide one:

@@ -269,17 +269,20 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
     if (any && warp == 0) {
       // =============================== copies =====================================
       const int shift = a.g.page_shift, per = WIDE_KEYS >> shift, page = 1 << shift;
-      int run = 0, n = 0;                    // chunks whose queries are on their way; tiles of all chunks
+      int run = 0, n = 0;                    // chunks; tiles of all chunks
       bool ok = true, more = true;
-      while (ok && more) {
-        if (run > 0 && !mbar_wait(bar(S::QE), (run - 1) & 1, s_abort, 211, true)) { ok = false; break; }
-        ++run;
-        if (lane == 0) {
+      auto queries = [&]() {
+        if (run > 1 && !mbar_wait(bar(S::QE), (run - 2) & 1, s_abort, 211, true)) { --run; return false; }
+        if (elect_one()) {
           mbar_expect_tx(bar(S::QF), (uint32_t)(2 * 128 * G * T));
           tma_load_3d(base, &tm_q, bar(S::QF), 0, w.h * G, w.g.tok0 + w.chunk * T);
           tma_load_3d(base + S::Q_HALF, &tm_q, bar(S::QF), 64, w.h * G, w.g.tok0 + w.chunk * T);
         }
         __syncwarp();
+        return true;
+      };
+      while (ok && more) {
+        if (++run == 1) queries();           // later ones go behind their first K: their room is free only when all S before are there
         const int32_t* row = a.g.table + (int64_t)w.g.slot * a.g.max_pages;
         const int last = w.g.pfx >> shift;   // pages of the prefix
         int first = w.tile * per;            // page numbers of 32 pages a lane each, and of the 32 after them
@@ -306,6 +309,11 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
               tma_load_2d(kd + x * page * 128, &tm_k, kbar, 0, r);
               if (!FP8) tma_load_2d(kd + TILE_HALF + x * page * 128, &tm_k, kbar, 64, r);
             }
+          }
+          if (t == w.tile && run > 1 && !queries()) {
+            ok = false;
+            ++n;                             // K of this tile is in flight
+            break;
           }
           if (!mbar_wait(bar(S::VE + vs), ((n / S::V_RING) & 1) ^ 1, s_abort, 213, true)) {
             ok = false;
