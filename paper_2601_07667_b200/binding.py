@@ -542,10 +542,12 @@ class Batch:
             raise AslError(ASL_ERR_INVALID, "batch: cu_q has one entry more than slots")
         self.n_tokens, self.n_q_heads = int(n_tokens), n_q_heads
         self.desc = AslBatch(len(self.slots), self.n_tokens, _ptr(self.slots), _ptr(self.cu_q))
-        self.workspace, self.ws_bytes = None, 0
+        self.ref = C.byref(self.desc)
+        self.workspace, self.ws, self.ws_bytes = None, 0, 0
         if n_q_heads is not None:
             self.ws_bytes = asl_attend_workspace(cache.ctx, cache.pages, self.desc, n_q_heads)
             self.workspace = cache.torch.empty(self.ws_bytes, dtype=cache.torch.uint8, device=cache.dev)
+            self.ws = self.workspace.data_ptr()
 
 
 class PagedCache:
@@ -573,6 +575,7 @@ class PagedCache:
             length = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
             refs = torch.zeros(n_pages, dtype=torch.int32, device=dev)
         self.dev, self.ctx = k.device, 0
+        self._i32, self._device, self._strides = torch.int32, k.get_device(), {}
         if k.dim() != 5 or v.shape != k.shape or k.shape[3] != page_size or v.dtype != torch.bfloat16 or table.dim() != 2:
             raise AslError(ASL_ERR_INVALID, "PagedCache: k and v are [n_layers][n_pages][H_k][page_size][d]")
         if k.element_size() == 1:
@@ -599,25 +602,30 @@ class PagedCache:
         self.pages.scratch_bytes = asl_pages_scratch(self.pages)
         self.scratch = torch.empty(self.pages.scratch_bytes, dtype=torch.uint8, device=self.dev)
         self.pages.scratch = _ptr(self.scratch)
-        self.ctx = asl_create(self.dev.index or 0)
+        self._ref, self._slots, self._d, self._k_bytes = C.byref(self.pages), table.shape[0], k.shape[4], k.element_size()
+        self.ctx = asl_create(self._device)
 
     def _ints(self, x, what: str):
-        if x.dtype != self.torch.int32 or not x.is_contiguous() or x.device != self.dev:
+        if x.dtype is not self._i32 or not x.is_contiguous() or x.get_device() != self._device:
             raise AslError(ASL_ERR_INVALID, f"{what}: dense int32 on the cache's device")
         return x
 
-    def _per_slot(self, x, what: str):
-        if x.numel() != self.pages.max_seqs:
+    def _per_slot(self, x, what: str) -> int:
+        if x.numel() != self._slots:
             raise AslError(ASL_ERR_INVALID, f"{what}: one value per slot")
-        return self._ints(x, what)
+        return self._ints(x, what).data_ptr()
 
     def _rows(self, x, what: str, n_tokens: int, heads: int, bytes_: int = 2):
         """A [tokens][heads][d] tensor's strides."""
-        if x.dim() != 3 or x.shape[0] < n_tokens or x.shape[1] != heads or x.shape[2] != self.pages.head_dim or x.stride(2) != 1:
+        if x.dim() != 3 or x.shape[0] < n_tokens or x.shape[1] != heads or x.shape[2] != self._d or x.stride(2) != 1:
             raise AslError(ASL_ERR_INVALID, f"{what}: [tokens][heads][d] with dense rows")
-        if x.element_size() != bytes_ or x.device != self.dev:
+        if x.element_size() != bytes_ or x.get_device() != self._device:
             raise AslError(ASL_ERR_INVALID, f"{what}: element type or device")
-        return x.stride(0), x.stride(1)
+        key = (x.stride(0), x.stride(1))
+        got = self._strides.get(key)
+        if got is None:
+            got = self._strides[key] = (C.c_int64 * 2)(*key)
+        return got
 
     def batch(self, slots, cu_q, n_tokens: int, n_q_heads: Optional[int] = None) -> Batch:
         """Sequences of a step: entry i is slot ``slots[i]`` (-1: padding) and owns tokens ``cu_q[i]`` .. ``cu_q[i+1]``, its last ones
@@ -625,47 +633,58 @@ class PagedCache:
         return Batch(self, slots, cu_q, n_tokens, n_q_heads)
 
     def reserve(self, want) -> None:
-        asl_pages_reserve(self.ctx, self.pages, self._per_slot(want, "want"))
+        """Slot s grows to ``want[s]`` tokens (negative, or no more than it has: left alone)."""
+        _check(_lib.asl_pages_reserve(self.ctx, self._ref, self._per_slot(want, "want"), _current_stream()), "asl_pages_reserve")
 
     def fork(self, parent) -> None:
-        asl_pages_fork(self.ctx, self.pages, self._per_slot(parent, "parent"))
+        """Slot s becomes a second holder of ``parent[s]``'s pages (negative: left alone)."""
+        _check(_lib.asl_pages_fork(self.ctx, self._ref, self._per_slot(parent, "parent"), _current_stream()), "asl_pages_fork")
 
     def trim(self, to) -> None:
-        asl_pages_trim(self.ctx, self.pages, self._per_slot(to, "to"))
+        """Slot s is cut to ``to[s]`` tokens, 0 frees it (negative: left alone)."""
+        _check(_lib.asl_pages_trim(self.ctx, self._ref, self._per_slot(to, "to"), _current_stream()), "asl_pages_trim")
 
     def store(self, layer: int, path: LayerPath, k, v, idx, slots) -> None:
-        """The kept rows of ``path``'s requests (``idx`` as its top-k wrote them) into layer ``layer`` of the slots."""
-        asl_pages_store(path.ctx, self.pages, layer, k, v, self._ints(idx, "idx"), self._ints(slots, "slots"))
+        """The kept rows of ``path``'s requests (``idx`` [H_k][sum_kept] as its top-k wrote them) into layer ``layer`` of the slots."""
+        if idx.numel() != path.H_k * path.sum_kept or slots.numel() != path.batch:
+            raise AslError(ASL_ERR_INVALID, "store: idx is [H_k][sum_kept], slots one per request")
+        _check(_lib.asl_pages_store(path.ctx, self._ref, layer, k.data_ptr(), v.data_ptr(), self._ints(idx, "idx").data_ptr(),
+                                    self._ints(slots, "slots").data_ptr(), _current_stream()), "asl_pages_store")
 
     def compact(self, layer: int, src, dst, off, idx, max_kept: int) -> None:
         """Token r of slot ``dst[j]`` gets row ``idx[h][off[j] + r]`` of slot ``src[j]``; ``idx`` [H_k][kept of all jobs]."""
-        if idx.dim() != 2 or idx.shape[0] != self.pages.n_kv_heads or len(off) != len(src) + 1 or len(dst) != len(src):
+        n = src.numel()
+        if idx.dim() != 2 or idx.shape[0] != self.pages.n_kv_heads or off.numel() != n + 1 or dst.numel() != n:
             raise AslError(ASL_ERR_INVALID, "compact: idx is [H_k][sum_kept], off has one entry more than src and dst")
-        asl_pages_compact(self.ctx, self.pages, layer, self._ints(src, "src"), self._ints(dst, "dst"), self._ints(off, "off"),
-                          len(src), self._ints(idx, "idx"), idx.shape[1], max_kept)
+        _check(_lib.asl_pages_compact(self.ctx, self._ref, layer, self._ints(src, "src").data_ptr(), self._ints(dst, "dst").data_ptr(),
+                                      self._ints(off, "off").data_ptr(), n, self._ints(idx, "idx").data_ptr(), idx.shape[1], max_kept,
+                                      _current_stream()), "asl_pages_compact")
 
     def append(self, layer: int, batch: Batch, k_new, v_new) -> None:
         """K and V rows [n_tokens][H_k][d] of the batch's tokens, to the ends of their sequences."""
-        H = self.pages.n_kv_heads
-        ks = self._rows(k_new, "k_new", batch.n_tokens, H, self.k.element_size())
-        vs = self._rows(v_new, "v_new", batch.n_tokens, H)
-        asl_pages_append(self.ctx, self.pages, layer, batch.desc, k_new, v_new, ks, vs)
+        ks = self._rows(k_new, "k_new", batch.n_tokens, self.pages.n_kv_heads, self._k_bytes)
+        vs = self._rows(v_new, "v_new", batch.n_tokens, self.pages.n_kv_heads)
+        _check(_lib.asl_pages_append(self.ctx, self._ref, layer, batch.ref, k_new.data_ptr(), v_new.data_ptr(), ks, vs,
+                                     _current_stream()), "asl_pages_append")
 
     def plan(self, batch: Batch, share: bool = True) -> None:
         """Deals out the attention of the step; again whenever lengths, pages or the batch have changed."""
-        asl_attend_plan(self.ctx, self.pages, batch.desc, batch.n_q_heads or 0, share, batch.workspace, batch.ws_bytes)
+        _check(_lib.asl_attend_plan(self.ctx, self._ref, batch.ref, batch.n_q_heads or 0, 1 if share else 0, batch.ws, batch.ws_bytes,
+                                    _current_stream()), "asl_attend_plan")
 
     def attend(self, layer: int, batch: Batch, q, out=None, lse=None):
         """Attention of the batch's tokens, q [n_tokens][H_q][d] bf16, over their sequences; out likewise (dense), lse
         [n_tokens][H_q] fp32 or None.  Returns out."""
-        strides = self._rows(q, "q", batch.n_tokens, batch.n_q_heads or 0)
+        heads, n = batch.n_q_heads or 0, batch.n_tokens
+        strides = self._rows(q, "q", n, heads)
         if out is None:
-            out = self.torch.empty((batch.n_tokens, batch.n_q_heads, self.pages.head_dim), dtype=q.dtype, device=self.dev)
-        elif not out.is_contiguous() or out.numel() < batch.n_tokens * batch.n_q_heads * self.pages.head_dim or out.element_size() != 2:
+            out = self.torch.empty((n, heads, self._d), dtype=q.dtype, device=self.dev)
+        elif not out.is_contiguous() or out.numel() < n * heads * self._d or out.element_size() != 2 or out.get_device() != self._device:
             raise AslError(ASL_ERR_INVALID, "out: dense [n_tokens][H_q][d] bf16")
-        if lse is not None and (not lse.is_contiguous() or lse.numel() < batch.n_tokens * batch.n_q_heads or lse.element_size() != 4):
+        if lse is not None and (not lse.is_contiguous() or lse.numel() < n * heads or lse.element_size() != 4 or lse.get_device() != self._device):
             raise AslError(ASL_ERR_INVALID, "lse: dense [n_tokens][H_q] fp32")
-        asl_attend(self.ctx, self.pages, layer, batch.desc, batch.n_q_heads, q, strides, out, lse, batch.workspace, batch.ws_bytes)
+        _check(_lib.asl_attend(self.ctx, self._ref, layer, batch.ref, heads, q.data_ptr(), strides, out.data_ptr(),
+                               0 if lse is None else lse.data_ptr(), batch.ws, batch.ws_bytes, _current_stream()), "asl_attend")
         return out
 
     def check(self) -> None:

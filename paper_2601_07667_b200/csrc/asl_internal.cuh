@@ -63,6 +63,7 @@ struct asl_ctx {
   bool topk_one_cta = false;          // the per-head top-k runs as one CTA per segment (asl_topk_plan)
   AslWorkspace ws{};
   int64_t launches = 0;
+  bool attend_ready = false;          // the attention kernels have been given their shared memory on the context's device
   // asl_run_layer: order between a layer's streams, and when the buffers of a slot are free again
   cudaEvent_t ev_scored = nullptr, ev_pooled = nullptr, ev_done[2][2] = {};
   bool pending[2] = {false, false};   // the slot's ev_done have been recorded since asl_run_reset

@@ -466,6 +466,12 @@ asl_status check_attend(const asl_ctx* c, const asl_pages* p, const asl_batch* b
   return ASL_OK;
 }
 
+// Whether neighbours could share enough, by the sizes alone, for the plan to look and the prefixes' kernel to be launched.
+bool may_share(const asl_pages* p, const asl_batch* b) {
+  const double row = (double)p->n_kv_heads * p->head_dim * (p->k_dtype == ASL_K_FP8_E4M3 ? 3 : 4);
+  return (double)(b->n_seqs - 1) * p->max_pages * p->page_size * row >= SHARE_MIN_BYTES;
+}
+
 }  // namespace
 
 extern "C" {
@@ -491,7 +497,7 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   a.w = ptrs_of(l, workspace);
   a.G = n_q_heads / p->n_kv_heads;
   a.n_q_heads = n_q_heads;
-  a.share = !(share && b->n_seqs > 1) ? 0 : (int64_t)b->n_seqs * p->max_pages > SAME_INSIDE ? 1 : 2;
+  a.share = !(share && may_share(p, b)) ? 0 : (int64_t)b->n_seqs * p->max_pages > SAME_INSIDE ? 1 : 2;
   a.narrow_grid = l.narrow_grid;
   a.wide_grid = l.wide_grid;
   const size_t smem = sizeof(int32_t) * (12 * (size_t)b->n_seqs + 2);
@@ -534,7 +540,11 @@ asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_b
   a.n_tokens = b->n_tokens;
   a.n_seqs = b->n_seqs;
   a.scale_log2 = (float)(1.4426950408889634 / sqrt((double)p->head_dim));
-  const bool wide = b->n_seqs > 1;       // neighbours may share (the plan says whether they do)
+  if (!c->attend_ready) {
+    if ((s = asl_attend_narrow_ready()) != ASL_OK || (s = asl_attend_wide_ready()) != ASL_OK) return s;
+    c->attend_ready = true;
+  }
+  const bool wide = may_share(p, b);     // (the plan says whether they do)
   if (wide) {
     s = asl_launch_attend_wide(c, p, a, l.wide_grid, st);
     if (s != ASL_OK) return s;

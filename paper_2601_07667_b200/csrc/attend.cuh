@@ -157,3 +157,6 @@ __device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
 // `beside`: right behind the prefixes' kernel, whose end it does not wait for
 asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, const AttendArgs& a, int grid, bool beside, cudaStream_t st);
 asl_status asl_launch_attend_wide(asl_ctx* c, const asl_pages* p, const AttendArgs& a, int grid, cudaStream_t st);
+// The kernels' shared memory on the current device, once per context.
+asl_status asl_attend_narrow_ready();
+asl_status asl_attend_wide_ready();

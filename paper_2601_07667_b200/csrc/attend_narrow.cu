@@ -379,9 +379,14 @@ asl_status asl_launch_attend_narrow(asl_ctx* c, const asl_pages* p, const Attend
   if (!k_map || !asl_make_map(&tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.g.v, 3, dims, strides, box)) return ASL_ERR_CUDA;
   auto kernel = fp8 ? attend_narrow_kernel<true> : attend_narrow_kernel<false>;
   const int smem = fp8 ? NarrowSmem<true>::BYTES : NarrowSmem<false>::BYTES;
-  ASL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   launch_after_smem(kernel, dim3(grid), dim3(WARPS * 32 + 32), smem, st, tm_k, tm_v, a, beside);
   c->launches += 1;
   ASL_CUDA(cudaGetLastError());
+  return ASL_OK;
+}
+
+asl_status asl_attend_narrow_ready() {
+  ASL_CUDA(cudaFuncSetAttribute(attend_narrow_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, NarrowSmem<false>::BYTES));
+  ASL_CUDA(cudaFuncSetAttribute(attend_narrow_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, NarrowSmem<true>::BYTES));
   return ASL_OK;
 }

@@ -494,9 +494,14 @@ asl_status asl_launch_attend_wide(asl_ctx* c, const asl_pages* p, const AttendAr
   if (!asl_make_map(&tm_v, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, a.g.v, 2, dims, vs, vbox)) return ASL_ERR_CUDA;
   auto kernel = fp8 ? attend_wide_kernel<true> : attend_wide_kernel<false>;
   const int smem = fp8 ? WideSmem<true>::BYTES : WideSmem<false>::BYTES;
-  ASL_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
   launch_after_smem(kernel, dim3(grid), dim3(fp8 ? WideSmem<true>::THREADS : WideSmem<false>::THREADS), smem, st, tm_q, tm_k, tm_v, a);
   c->launches += 1;
   ASL_CUDA(cudaGetLastError());
+  return ASL_OK;
+}
+
+asl_status asl_attend_wide_ready() {
+  ASL_CUDA(cudaFuncSetAttribute(attend_wide_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, WideSmem<false>::BYTES));
+  ASL_CUDA(cudaFuncSetAttribute(attend_wide_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, WideSmem<true>::BYTES));
   return ASL_OK;
 }
