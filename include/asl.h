@@ -366,7 +366,7 @@ typedef struct {
   int32_t k_dtype;        /* ASL_K_BF16, or ASL_K_FP8_E4M3: K holds codes, the key is code x k_scale[layer][kv head] */
   void* k;                /* device [n_layers][n_pages][H_k][page_size][d], bf16 or E4M3 codes, 16-byte aligned */
   void* v;                /* device, the same in bf16                                            */
-  const float* k_scale;   /* device [n_layers][H_k]; read only for ASL_K_FP8_E4M3                */
+  const float* k_scale;   /* device [n_layers][H_k], finite and > 0; read only for ASL_K_FP8_E4M3 */
   int32_t* table;         /* device [max_seqs][max_pages]                                        */
   int32_t* len;           /* device [max_seqs]                                                   */
   int32_t* refs;          /* device [n_pages]                                                    */
@@ -382,7 +382,8 @@ typedef struct {
   int32_t n_seqs;         /* at most 4096                                                        */
   int32_t n_tokens;       /* rows that the buffers have room for; cu_q[n_seqs] <= n_tokens       */
   const int32_t* slots;   /* device [n_seqs], each slot once                                     */
-  const int32_t* cu_q;    /* device [n_seqs + 1], cu_q[0] = 0, ascending                         */
+  const int32_t* cu_q;    /* device [n_seqs + 1], from 0 on, ascending (an asl_attend_plan that  */
+                          /* finds them otherwise is refused and noted with slot -1)             */
 } asl_batch;
 
 /* Checks the description and reports the bytes of `scratch`.  ASL_ERR_INVALID, or ASL_ERR_UNSUPPORTED for a head_dim
@@ -443,7 +444,8 @@ asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, 
  * read once for all of them, their rows multiplied together; without it, or where little is shared, every sequence
  * reads its own.  The workspace (asl_attend_workspace bytes, 256-byte aligned) carries the plan and the parts of rows
  * whose keys are split over several blocks; calls that share it have to be ordered one behind another.
- * H_q is a multiple of H_k with H_q / H_k <= 128. */
+ * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its sizes writes nothing
+ * and notes ASL_ERR_WORKSPACE; after an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
 asl_status asl_attend_workspace(const asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, size_t* bytes);
 asl_status asl_attend_plan(asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, int32_t share,
                            void* workspace, size_t workspace_bytes, void* stream);

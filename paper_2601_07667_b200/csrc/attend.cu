@@ -82,7 +82,7 @@ struct PlanArgs {
 __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   extern __shared__ int32_t sm[];
   __shared__ int part[PLAN_THREADS / 32];
-  __shared__ int n_groups_s, any_full;
+  __shared__ int n_groups_s, any_full, bad;
   __shared__ unsigned long long most_s;
   pdl_wait_predecessor();
   const int tid = threadIdx.x, n = a.b.n_seqs, G = a.G, H = a.g.n_kv_heads;
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   int32_t* gchunk = sm + 9 * n;
   int32_t* first = sm + 10 * n;            // [n + 1] narrow tiles before
   int32_t* gcost = sm + 11 * n + 1;        // [n + 1] wide cost before
-  if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; }
+  if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; bad = 0; }
   for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tokens[t].seq.ntok = 0;
   __syncthreads();
   for (int i = tid; i < n; i += PLAN_THREADS) {
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     const int same = a.share == 1 ? __ldcg(a.w.same + i) : 0;
     const bool slot_ok = (unsigned)s < (unsigned)a.g.max_seqs, tok_ok = t0 >= 0 && t1 >= t0 && t1 <= a.b.n_tokens;
     const int l = slot_ok ? __ldcg(a.g.len + s) : 0;
-    if (slot_ok && !tok_ok) note_error(a.g.err, ASL_ERR_INVALID, s);
+    if (!tok_ok) bad = 1;                  // (tokens that two entries own would be more rows than the workspace has room for)
     const int m = slot_ok && tok_ok ? t1 - t0 : 0;
     ntok[i] = m;
     slot[i] = m ? s : -1;
@@ -117,8 +117,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     if (m) atomicAdd(&most_s, (unsigned long long)narrow_chunks_of(m, G) * (unsigned)(len[i] / NARROW_KEYS + 2));
   }
   __syncthreads();
-  if (most_s * H >= 1ull << 30) {
-    if (tid == 0) note_error(a.g.err, ASL_ERR_UNSUPPORTED, -1);
+  if (bad || most_s * H >= 1ull << 30) {
+    if (tid == 0) note_error(a.g.err, bad ? ASL_ERR_INVALID : ASL_ERR_UNSUPPORTED, -1);
     return;
   }
   if (a.share == 2) {                      // few pages: no launch of its own for what neighbours have in common, a warp a pair

@@ -264,7 +264,8 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
     at = o;
     if (o < 0 || (int64_t)o + kept > sum_kept) kept = 0;
     const bool fits = (unsigned)src < (unsigned)g.max_seqs && src != slot;
-    n_src = fits ? __ldcg(g.len + src) : 0;
+    n_src = fits ? min(__ldcg(g.len + src), g.max_pages << g.page_shift) : 0;
+    if (blockIdx.x == 0 && h == 0 && tid == 0 && kept > gridDim.x * R) note_error(g.err, ASL_ERR_INVALID, slot);     // more than max_kept
   } else {
     if (x.latch && asl_finished(x.latch + b, x.cur_layer)) return;
     const AslReq rq = x.req[b];
