@@ -12,6 +12,7 @@ namespace {
 
 constexpr int WARPS = 4;                   // that compute; one more copies
 constexpr int STAGES = 3;
+constexpr int Q_PITCH = 272;               // bytes from one query row to the next, so that eight of them lie in different banks
 constexpr int O_STRIDE = 68;               // floats from one row to the next where parts of four warps are joined
 
 template <bool FP8>
@@ -20,9 +21,12 @@ struct NarrowSmem {
   static constexpr int STAGE = K_BYTES + V_BYTES;
   static constexpr int JOIN = STAGES * STAGE;                       // float[4][8][O_STRIDE]
   static constexpr int ML = JOIN + WARPS * 8 * O_STRIDE * 4;        // float2[4][16]
-  static constexpr int BARS = ML + WARPS * 16 * 8;
-  static constexpr int MISC = BARS + 2 * STAGES * 8;
-  static constexpr int BYTES = MISC + 16 + 1024;                    // and the alignment of its base
+  static constexpr int Q = ML + WARPS * 16 * 8;                      // the next chunk's rows
+  static constexpr int PART = Q + NARROW_ROWS * Q_PITCH;            // what they are
+  static constexpr int BARS = PART + 64;
+  static constexpr int QF = 2 * STAGES, QE = QF + 1;
+  static constexpr int MISC = BARS + (QE + 1) * 8;
+  static constexpr int BYTES = MISC + 32 + 1024;                    // and the alignment of its base
 };
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
@@ -59,19 +63,23 @@ struct Walk {
     return true;
   }
   __device__ __forceinline__ int here() const { return min(nt - tile, left); }     // tiles of this part
+  // the sequence after this one, asked for early (the one before the last head's end is loaded for nothing)
+  __device__ __forceinline__ AttendSeq ahead(const AttendArgs& a) const { return load_seq(a.w.seqs + (i + 1 < items ? i + 1 : 0)); }
   // the next chunk; false at the end
-  __device__ __forceinline__ bool next(const AttendArgs& a) {
+  __device__ __forceinline__ bool next(const AttendArgs& a, const AttendSeq& coming) {
     left -= here();
     if (left <= 0) return false;
     tile = 0;
     if (++chunk < nch) return true;
     chunk = 0;
+    bool first = true;
     do {
       if (++i >= items) {
         i = 0;
         if (++h >= a.g.n_kv_heads) return false;
       }
-      s = load_seq(a.w.seqs + i);
+      s = first ? coming : load_seq(a.w.seqs + i);
+      first = false;
       sizes(a);
     } while (nch == 0);
     return true;
@@ -84,6 +92,14 @@ struct Walk {
   __device__ __forceinline__ int64_t slot() const { return (int64_t)h * chunks + s.chunk0 + chunk + blockIdx.x; }
 };
 
+// A part, as the copying warp describes it to the others.
+struct Part {
+  int32_t tok0, ntok, len, pfx, h, chunk, tile, tiles;   // tiles 0: there is none any more
+  int32_t sole, pad;
+  int64_t slot;
+};
+static_assert(sizeof(Part) <= 64, "room for a part's description");
+
 template <bool FP8>
 __global__ void __launch_bounds__(WARPS * 32 + 32, 2)
 attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, AttendArgs a, int beside) {
@@ -95,8 +111,12 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   volatile int* s_abort = reinterpret_cast<volatile int*>(sm + S::MISC);
   auto full = [&](int st) { return base + S::BARS + 8 * st; };
   auto empty = [&](int st) { return base + S::BARS + 8 * (STAGES + st); };
+  const uint32_t q_full = base + S::BARS + 8 * S::QF, q_empty = base + S::BARS + 8 * S::QE;
+  Part* part = reinterpret_cast<Part*>(sm + S::PART);
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), WARPS); }
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, WARPS);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -104,17 +124,38 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   // Behind the prefixes' kernel (`beside`) nothing is waited for: that kernel lets this one start only when all before it is
   // done, and neither writes what the other reads.
   if (!beside) pdl_wait_predecessor();
-  Walk w;
-  const int n_kv = a.g.n_kv_heads;
-  const bool any = w.begin(a);
-
-  if (any && warp == WARPS) {
+  const int n_kv = a.g.n_kv_heads, G = a.group_heads;
+  if (warp == WARPS) {
+    Walk w;
+    const bool any = w.begin(a);
     // ---- copies: tiles of whole pages' pieces; pages behind the sequence's end are not read ----
     const int piece = min(1 << a.g.page_shift, NARROW_KEYS), per = NARROW_KEYS / piece;
-    int n = 0;
-    bool more = true;
+    int n = 0, parts = 0;
+    bool more = any;
+    // rows and description of a part (null: there is none any more) to the others, who have taken over the one before
+    auto tell = [&](const Part& what, int rows) {
+      if (parts > 0 && !mbar_wait(q_empty, (parts - 1) & 1, s_abort, 204, true)) return false;
+      ++parts;
+      if (lane == 0) {
+        *part = what;
+        mbar_expect_tx(q_full, (uint32_t)(rows * 256));
+      }
+      __syncwarp();
+      if (lane < rows) {
+        const int lr = what.chunk * NARROW_ROWS + lane;
+        const __nv_bfloat16* q = a.q + (int64_t)(what.tok0 + lr / G) * a.qs_t + (int64_t)(what.h * G + lr % G) * a.qs_h;
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], 256, [%2];" ::"r"(base + S::Q + lane * Q_PITCH),
+                     "l"(q), "r"(q_full)
+                     : "memory");
+      }
+      __syncwarp();
+      return true;
+    };
     while (more) {
       const int nt = w.here();
+      const AttendSeq coming = w.ahead(a);
+      const Part what = {w.s.tok0, w.s.ntok, w.s.len, w.s.pfx, w.h, w.chunk, w.tile, nt, w.sole(), 0, w.slot()};
+      if (!tell(what, min(NARROW_ROWS, w.s.ntok * G - w.chunk * NARROW_ROWS))) break;
       const int32_t* row = a.g.table + (int64_t)w.s.slot * a.g.max_pages;
       const int end = min(pages_for(w.s.len, a.g.page_shift), a.g.max_pages);
       int ids = 0, first = -64;
@@ -143,49 +184,61 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           }
         }
       }
-      if (more) more = w.next(a);
+      if (more) more = w.next(a, coming);
     }
+    const Part none = {};
+    if (!*s_abort) tell(none, 0);
     if (*s_abort) {                                    // copies in flight land before the block ends
       for (int i = max(0, n - STAGES); i < n; ++i) mbar_wait(full(i % STAGES), (i / STAGES) & 1, s_abort, 202, false);
+      if (parts) mbar_wait(q_full, (parts - 1) & 1, s_abort, 205, false);
     }
-  } else if (any) {
+  } else {
     // ---- arithmetic ----
-    const int gid = lane >> 2, tig = lane & 3, G = a.group_heads;
+    const int gid = lane >> 2, tig = lane & 3;
     // where the rows that a lane loads lie in a stage: piece after piece, a piece's first halves before its second ones
     const int krow = warp * 16 + (lane >> 4) * 8 + (lane & 7), vrow = warp * 16 + ((lane >> 3) & 1) * 8 + (lane & 7);
     const int piece = min(1 << a.g.page_shift, NARROW_KEYS), half_bytes = piece * 128;
     const int k_at = (krow / piece * piece + krow) * 128, v_at = (vrow / piece * piece + vrow) * 128;
+    int* there = reinterpret_cast<int*>(sm + S::MISC + 16);
     int n = 0;
-    bool more = true;
-    while (more) {
-      const int nt = w.here();
+    for (int parts = 0;; ++parts) {
+      // (a part is begun by all four warps or by none: they meet at barriers until its end)
+      const bool here = mbar_wait(q_full, parts & 1, s_abort, 206, true);
+      if (lane == 0) there[warp] = here;
+      bar_sync(1, WARPS * 32);                         // and join and ml, of the part before, are free
+      if (!(there[0] && there[1] && there[2] && there[3])) break;
+      const Part w = *part;
+      if (w.tiles == 0) break;
+      const int nt = w.tiles;
       const float c = a.scale_log2 * (FP8 ? __ldg(a.k_scale + w.h) : 1.0f);
-      const int rows = w.s.ntok * G, lr0 = w.chunk * NARROW_ROWS;
-      // the chunk's rows gid and gid + 8: token, query head, keys it sees
+      const int rows = w.ntok * G, lr0 = w.chunk * NARROW_ROWS;
+      // the chunk's rows gid and gid + 8: token, keys it sees (rows that do not exist: none)
       int lim[2], tok[2];
       uint32_t qf[8][4];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int lr = lr0 + gid + 8 * i;
-        const bool ok = lr < rows;
         tok[i] = lr / G;
-        lim[i] = ok ? max(0, w.s.len - w.s.ntok + tok[i] + 1) : 0;
-        const __nv_bfloat16* q = a.q + (int64_t)(w.s.tok0 + tok[i]) * a.qs_t + (int64_t)(w.h * G + lr % G) * a.qs_h;
+        lim[i] = lr < rows ? max(0, w.len - w.ntok + tok[i] + 1) : 0;
+      }
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          if (FP8) {       // a lane's codes are four channels in a row: so are its queries'
-            const uint2 v = ok ? __ldg(reinterpret_cast<const uint2*>(q + ks * 16 + tig * 4)) : make_uint2(0, 0);
+      for (int ks = 0; ks < 8; ++ks) {
+        if (FP8) {         // a lane's codes are four channels in a row: so are its queries'
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint2 v = *reinterpret_cast<const uint2*>(sm + S::Q + (gid + 8 * i) * Q_PITCH + ks * 32 + tig * 8);
             qf[ks][i] = v.x;
             qf[ks][2 + i] = v.y;
-          } else {
-            qf[ks][i] = ok ? __ldg(reinterpret_cast<const uint32_t*>(q + ks * 16 + tig * 2)) : 0;
-            qf[ks][2 + i] = ok ? __ldg(reinterpret_cast<const uint32_t*>(q + ks * 16 + tig * 2 + 8)) : 0;
           }
+        } else {
+          ldsm4(base + S::Q + ((lane & 7) + ((lane >> 3) & 1) * 8) * Q_PITCH + ks * 32 + (lane >> 4) * 16, qf[ks]);
         }
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(q_empty);
       const int lr1 = min(lr0 + NARROW_ROWS, rows) - 1;                      // last row of the chunk
       const int tok_a = lr0 / G, tok_b = lr1 / G;
-      const int lim_a = max(0, w.s.len - w.s.ntok + tok_a + 1), lim_b = max(0, w.s.len - w.s.ntok + tok_b + 1);
+      const int lim_a = max(0, w.len - w.ntok + tok_a + 1), lim_b = max(0, w.len - w.ntok + tok_b + 1);
       float o[16][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
 #pragma unroll
       for (int j = 0; j < 16; ++j)
@@ -194,7 +247,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
 
       for (int t = 0; t < nt; ++t, ++n) {
         const int st = n % STAGES;
-        const int key0 = w.s.pfx + (w.tile + t) * NARROW_KEYS + warp * 16;
+        const int key0 = w.pfx + (w.tile + t) * NARROW_KEYS + warp * 16;
         mbar_wait(full(st), (n / STAGES) & 1, s_abort, 203, true);
         if (key0 < lim_b) {
           const uint32_t ks_ = base + st * S::STAGE, vs_ = ks_ + S::K_BYTES;
@@ -271,7 +324,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             // Keys that a row does not see count for nothing, whatever their V holds (0 x NaN would not): token by token with
             // the unseen keys' V cleared, and only that token's rows are taken.
             for (int tt = tok_a; tt <= tok_b; ++tt) {
-              const int see = w.s.len - w.s.ntok + tt + 1 - key0;               // of the warp's 16 keys
+              const int see = w.len - w.ntok + tt + 1 - key0;               // of the warp's 16 keys
               uint32_t keep[2];
 #pragma unroll
               for (int e = 0; e < 2; ++e)
@@ -309,8 +362,8 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         ml[warp * 16 + gid] = make_float2(m[0], l[0]);
         ml[warp * 16 + gid + 8] = make_float2(m[1], l[1]);
       }
-      const bool sole = w.sole();
-      const int64_t slot = w.slot();
+      const bool sole = w.sole;
+      const int64_t slot = w.slot;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (lr0 + 8 * i >= rows) break;
@@ -343,7 +396,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
             const int hc = half * 64 + ch;
             if (sole) {
               const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-              const int64_t row = (int64_t)(w.s.tok0 + lr / G) * a.n_q_heads + w.h * G + lr % G;
+              const int64_t row = (int64_t)(w.tok0 + lr / G) * a.n_q_heads + w.h * G + lr % G;
               const uint2 v = make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
               *reinterpret_cast<uint2*>(a.out + row * 128 + hc) = v;
               if (a.lse && half == 0 && ch == 0) a.lse[row] = (at + log2f(sum)) * 0.6931471805599453f;
@@ -354,8 +407,6 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           }
         }
       }
-      bar_sync(1, WARPS * 32);                         // ml and join are free
-      more = w.next(a);
     }
   }
   __syncthreads();
