@@ -439,10 +439,11 @@ asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, 
  * they hold, and so do positions after p.  A token that sees no key (a free slot) has out = 0 and lse = -inf.
  *
  * asl_attend_plan reads table, len and the batch on the device and deals the work out; every asl_attend of the step,
- * on any layer, uses it.  Plan again when a slot's length or pages, or the batch, have changed.  With `share` the plan
- * looks for neighbours of the batch whose pages begin alike (forks of one prompt, side by side) and such a prefix is
- * read once for all of them, their rows multiplied together; without it, or where little is shared, every sequence
- * reads its own.  The workspace (asl_attend_workspace bytes, 256-byte aligned) carries the plan and the parts of rows
+ * on any layer, uses it.  Plan again when a slot's length or pages, or the batch, have changed.  With `share` 1 the plan
+ * looks for neighbours of the batch whose pages begin alike (forks of one prompt, side by side) and, where that saves
+ * enough, such a prefix is read once for all of them, their rows multiplied together; with 2 wherever a page is
+ * shared; with 0 every sequence reads its own.  asl_attend is given the plan's `share`; its kernels follow one another on
+ * the stream, so that no other thread may launch on it meanwhile.  The workspace (asl_attend_workspace bytes, 256-byte aligned) carries the plan and the parts of rows
  * whose keys are split over several blocks; calls that share it have to be ordered one behind another.
  * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its sizes writes nothing
  * and notes ASL_ERR_WORKSPACE; after an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
@@ -452,7 +453,7 @@ asl_status asl_attend_plan(asl_ctx* ctx, const asl_pages* pages, const asl_batch
 /* q: device bf16 [n_tokens][H_q][d] (element strides token, head: multiples of 8); out: device bf16 dense
  * [n_tokens][H_q][d]; lse: device fp32 [n_tokens][H_q], or null. */
 asl_status asl_attend(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const asl_batch* batch, int32_t n_q_heads,
-                      const void* q, const int64_t q_stride[2], void* out, float* lse, void* workspace,
+                      int32_t share, const void* q, const int64_t q_stride[2], void* out, float* lse, void* workspace,
                       size_t workspace_bytes, void* stream);
 
 /* asl_run_layer with its last step into pages: asl_pages_store on `side2` in asl_compact_kv's place (k_out and v_out of

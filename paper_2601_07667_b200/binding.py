@@ -115,7 +115,7 @@ def _load() -> C.CDLL:
     lib.asl_pages_status.argtypes = [vp, pages, vp, C.POINTER(i32)]
     lib.asl_attend_workspace.argtypes = [vp, pages, batch, i32, C.POINTER(sz)]
     lib.asl_attend_plan.argtypes = [vp, pages, batch, i32, i32, vp, sz, vp]
-    lib.asl_attend.argtypes = [vp, pages, i32, batch, i32, vp, two, vp, vp, vp, sz, vp]
+    lib.asl_attend.argtypes = [vp, pages, i32, batch, i32, i32, vp, two, vp, vp, vp, sz, vp]
     lib.asl_run_layer_pages.argtypes = [vp, C.POINTER(AslLayer), pages, i32, vp, vp, vp, vp, vp, i32, i32, i32]
     lib.asl_launch_count.argtypes = [vp]
     lib.asl_launch_count.restype = i64
@@ -344,15 +344,15 @@ def asl_attend_workspace(ctx, pages: AslPages, batch: AslBatch, n_q_heads: int) 
     return size.value
 
 
-def asl_attend_plan(ctx, pages: AslPages, batch: AslBatch, n_q_heads: int, share: bool, workspace, workspace_bytes: int,
+def asl_attend_plan(ctx, pages: AslPages, batch: AslBatch, n_q_heads: int, share: int, workspace, workspace_bytes: int,
                     stream=None) -> None:
     _check(_lib.asl_attend_plan(ctx, pages, batch, int(n_q_heads), int(share), _ptr(workspace), int(workspace_bytes),
                                 _stream_handle(stream)), "asl_attend_plan")
 
 
-def asl_attend(ctx, pages: AslPages, layer: int, batch: AslBatch, n_q_heads: int, q, q_stride, out, lse, workspace,
+def asl_attend(ctx, pages: AslPages, layer: int, batch: AslBatch, n_q_heads: int, share: int, q, q_stride, out, lse, workspace,
                workspace_bytes: int, stream=None) -> None:
-    _check(_lib.asl_attend(ctx, pages, int(layer), batch, int(n_q_heads), _ptr(q), (C.c_int64 * 2)(*q_stride), _ptr(out), _ptr(lse),
+    _check(_lib.asl_attend(ctx, pages, int(layer), batch, int(n_q_heads), int(share), _ptr(q), (C.c_int64 * 2)(*q_stride), _ptr(out), _ptr(lse),
                            _ptr(workspace), int(workspace_bytes), _stream_handle(stream)), "asl_attend")
 
 
@@ -543,7 +543,7 @@ class Batch:
         self.n_tokens, self.n_q_heads = int(n_tokens), n_q_heads
         self.desc = AslBatch(len(self.slots), self.n_tokens, _ptr(self.slots), _ptr(self.cu_q))
         self.ref = C.byref(self.desc)
-        self.workspace, self.ws, self.ws_bytes = None, 0, 0
+        self.workspace, self.ws, self.ws_bytes, self.share = None, 0, 0, 1
         if n_q_heads is not None:
             self.ws_bytes = asl_attend_workspace(cache.ctx, cache.pages, self.desc, n_q_heads)
             self.workspace = cache.torch.empty(self.ws_bytes, dtype=cache.torch.uint8, device=cache.dev)
@@ -667,9 +667,11 @@ class PagedCache:
         _check(_lib.asl_pages_append(self.ctx, self._ref, layer, batch.ref, k_new.data_ptr(), v_new.data_ptr(), ks, vs,
                                      _current_stream()), "asl_pages_append")
 
-    def plan(self, batch: Batch, share: bool = True) -> None:
-        """Deals out the attention of the step; again whenever lengths, pages or the batch have changed."""
-        _check(_lib.asl_attend_plan(self.ctx, self._ref, batch.ref, batch.n_q_heads or 0, 1 if share else 0, batch.ws, batch.ws_bytes,
+    def plan(self, batch: Batch, share: int = 1) -> None:
+        """Deals out the attention of the step; again whenever lengths, pages or the batch have changed.  Prefixes that neighbours
+        share are read once for all of them with ``share`` 1 where that saves enough, 2 wherever there are any, 0 nowhere."""
+        batch.share = int(share)
+        _check(_lib.asl_attend_plan(self.ctx, self._ref, batch.ref, batch.n_q_heads or 0, batch.share, batch.ws, batch.ws_bytes,
                                     _current_stream()), "asl_attend_plan")
 
     def attend(self, layer: int, batch: Batch, q, out=None, lse=None):
@@ -683,7 +685,7 @@ class PagedCache:
             raise AslError(ASL_ERR_INVALID, "out: dense [n_tokens][H_q][d] bf16")
         if lse is not None and (not lse.is_contiguous() or lse.numel() < n * heads or lse.element_size() != 4 or lse.get_device() != self._device):
             raise AslError(ASL_ERR_INVALID, "lse: dense [n_tokens][H_q] fp32")
-        _check(_lib.asl_attend(self.ctx, self._ref, layer, batch.ref, heads, q.data_ptr(), strides, out.data_ptr(),
+        _check(_lib.asl_attend(self.ctx, self._ref, layer, batch.ref, heads, batch.share, q.data_ptr(), strides, out.data_ptr(),
                                0 if lse is None else lse.data_ptr(), batch.ws, batch.ws_bytes, _current_stream()), "asl_attend")
         return out
 

@@ -74,6 +74,7 @@ struct PlanArgs {
   asl_batch b;
   AttendPtrs w;
   int32_t G, n_q_heads, narrow_grid, wide_grid;
+  float min_bytes;         // that groups' prefixes have to save
   int32_t share;           // 0: nothing is; what neighbours have in common comes from 1: attend_same_kernel, 2: the plan itself
 };
 
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       gpfx[ng - 1] = held > 1 ? keys : 0;
       saved += (float)(held - 1) * keys;
     }
-    if (saved * H * (a.g.k_row + a.g.v_row) < SHARE_MIN_BYTES)
+    if (saved * H * (a.g.k_row + a.g.v_row) < a.min_bytes)
       for (int g = 0; g < ng; ++g) gpfx[g] = 0;
     n_groups_s = ng;
   }
@@ -467,9 +468,9 @@ asl_status check_attend(const asl_ctx* c, const asl_pages* p, const asl_batch* b
 }
 
 // Whether neighbours could share enough, by the sizes alone, for the plan to look and the prefixes' kernel to be launched.
-bool may_share(const asl_pages* p, const asl_batch* b) {
-  const double row = (double)p->n_kv_heads * p->head_dim * (p->k_dtype == ASL_K_FP8_E4M3 ? 3 : 4);
-  return (double)(b->n_seqs - 1) * p->max_pages * p->page_size * row >= SHARE_MIN_BYTES;
+bool may_share(const asl_pages* p, const asl_batch* b, int share) {
+  if (share == 0 || b->n_seqs < 2) return false;
+  return share == 2 || (double)(b->n_seqs - 1) * p->max_pages * p->page_size * p->n_kv_heads * p->head_dim * 4 >= SHARE_MIN_BYTES;
 }
 
 }  // namespace
@@ -487,7 +488,7 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
                            size_t workspace_bytes, void* stream) {
   const asl_status s = check_attend(c, p, b, n_q_heads);
   if (s != ASL_OK) return s;
-  if (!asl_on_device(c)) return ASL_ERR_INVALID;
+  if (!asl_on_device(c) || share < 0 || share > 2) return ASL_ERR_INVALID;
   const AttendLayout l = layout_of(c->sm_count, p->n_kv_heads, b->n_seqs, b->n_tokens, n_q_heads);
   if (!workspace || workspace_bytes < l.total || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return ASL_ERR_WORKSPACE;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -497,9 +498,10 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   a.w = ptrs_of(l, workspace);
   a.G = n_q_heads / p->n_kv_heads;
   a.n_q_heads = n_q_heads;
-  a.share = !(share && may_share(p, b)) ? 0 : (int64_t)b->n_seqs * p->max_pages > SAME_INSIDE ? 1 : 2;
+  a.share = !may_share(p, b, share) ? 0 : (int64_t)b->n_seqs * p->max_pages > SAME_INSIDE ? 1 : 2;
   a.narrow_grid = l.narrow_grid;
   a.wide_grid = l.wide_grid;
+  a.min_bytes = share == 2 ? 0.0f : SHARE_MIN_BYTES;
   const size_t smem = sizeof(int32_t) * (12 * (size_t)b->n_seqs + 2);
   if (smem > 48 * 1024)
     ASL_CUDA(cudaFuncSetAttribute(attend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (12 * ATTEND_MAX_SEQS + 2)));
@@ -513,11 +515,11 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   return ASL_OK;
 }
 
-asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_batch* b, int32_t n_q_heads, const void* q,
-                      const int64_t q_stride[2], void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_batch* b, int32_t n_q_heads, int32_t share,
+                      const void* q, const int64_t q_stride[2], void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
   asl_status s = check_attend(c, p, b, n_q_heads);
   if (s != ASL_OK) return s;
-  if (!asl_on_device(c)) return ASL_ERR_INVALID;
+  if (!asl_on_device(c) || share < 0 || share > 2) return ASL_ERR_INVALID;
   if (layer < 0 || layer >= p->n_layers || !q || !out || !q_stride || !asl_aligned16(q) || !asl_aligned16(out)) return ASL_ERR_INVALID;
   for (int i = 0; i < 2; ++i)
     if (q_stride[i] < p->head_dim || q_stride[i] % 8) return ASL_ERR_INVALID;
@@ -544,7 +546,8 @@ asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_b
     if ((s = asl_attend_narrow_ready()) != ASL_OK || (s = asl_attend_wide_ready()) != ASL_OK) return s;
     c->attend_ready = true;
   }
-  const bool wide = may_share(p, b);     // (the plan says whether they do)
+  const bool wide = may_share(p, b, share);        // (the plan says whether they do)
+  a.with_wide = wide;
   if (wide) {
     s = asl_launch_attend_wide(c, p, a, l.wide_grid, st);
     if (s != ASL_OK) return s;

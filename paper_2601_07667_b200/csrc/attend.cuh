@@ -68,6 +68,7 @@ struct AttendArgs {
   const float* k_scale;    // [H_k] of the layer, or null
   int32_t* err;            // the context's word of bounded waits
   int32_t n_q_heads, group_heads, n_tokens, n_seqs;
+  int32_t with_wide;       // the prefixes' kernel is launched
   float scale_log2;
 };
 
@@ -90,10 +91,11 @@ __device__ __forceinline__ AttendHead load_head(const AttendHead* h) {
   }
   return r;
 }
-// A workspace that holds no plan, or one for other sizes, is refused before anything is read through it.
+// A workspace that holds no plan, or one for other sizes, is refused before anything is read through it, and so is one with
+// shared prefixes where their kernel is not launched.
 __device__ __forceinline__ bool plan_fits(const AttendArgs& a, const AttendHead& h) {
   const bool fits = h.mark == ATTEND_MARK && h.n_seqs == a.n_seqs && h.n_tokens == a.n_tokens && h.n_q_heads == a.n_q_heads &&
-                    h.n_kv_heads == a.g.n_kv_heads;
+                    h.n_kv_heads == a.g.n_kv_heads && (h.wide_cost == 0 || a.with_wide);
   if (!fits && threadIdx.x == 0) note_error(a.g.err, ASL_ERR_WORKSPACE, -1);
   return fits;
 }

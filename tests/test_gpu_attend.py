@@ -21,7 +21,7 @@ def test_single_tokens(heads, page, fp8):
     both.fill(lens)
     slots = [int(x) for x in np.random.default_rng(1).permutation(len(lens))]
     check_attention(both, 0, slots, list(range(len(lens) + 1)), heads[0], share=False)
-    check_attention(both, 0, slots, list(range(len(lens) + 1)), heads[0], share=True, want_lse=False)
+    check_attention(both, 0, slots, list(range(len(lens) + 1)), heads[0], share=2, want_lse=False)
 
 
 @pytest.mark.parametrize("heads", [(8, 2), (28, 4), (32, 1), (6, 6)])
@@ -34,7 +34,7 @@ def test_several_tokens_of_a_sequence(heads, page, fp8):
     both.fill(lens + [0])
     slots = [0, 1, 2, 3, 4, 5, 6, 7, -1, 99]
     cu = np.concatenate([[0], np.cumsum(counts + [3, 2])]).tolist()
-    check_attention(both, 0, slots, cu, heads[0], share=True, n_tokens=cu[-1] + 4)
+    check_attention(both, 0, slots, cu, heads[0], share=2, n_tokens=cu[-1] + 4)
 
 
 def test_keys_that_are_not_seen_may_hold_anything():
@@ -85,7 +85,7 @@ def test_strided_queries_and_layers():
     wide = torch.randn((5, 3, 20, 128), device="cuda").to(torch.bfloat16)           # q between other tensors of a fused projection
     for layer in range(3):
         q = wide[:, layer, 4:16]
-        check_attention(both, layer, [2, 0, 1], [0, 2, 3, 5], 12, share=True, q=(q, q.double().cpu().numpy()))
+        check_attention(both, layer, [2, 0, 1], [0, 2, 3, 5], 12, share=2, q=(q, q.double().cpu().numpy()))
 
 
 def test_the_same_bits_every_time():
@@ -132,7 +132,7 @@ def test_a_shared_prefix(heads, page, fp8):
     """Nine sequences on one prompt whose last page is not full and whose last tile is not either."""
     prompt = 128 * 5 + max(page, 48) + 5
     both, slots = forked(heads, page, [prompt], [[1, 2, 15, 60, 64, 65, 130, 7, 1]], fp8=fp8, seed=page)
-    check_attention(both, 0, slots, list(range(10)), heads[0], share=True)
+    check_attention(both, 0, slots, list(range(10)), heads[0], share=2)
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -140,7 +140,7 @@ def test_a_shared_prefix(heads, page, fp8):
 def test_rows_around_a_chunk(heads, n, fp8):
     """Rows of a prefix below, at and above 128 and 256."""
     both, slots = forked(heads, 32, [1056], [[1 + (i * 7) % 40 for i in range(n)]], fp8=fp8, seed=n)
-    check_attention(both, 0, slots, list(range(n + 1)), heads[0], share=True)
+    check_attention(both, 0, slots, list(range(n + 1)), heads[0], share=2)
 
 
 @pytest.mark.parametrize("fp8", [False, True])
@@ -153,9 +153,9 @@ def test_several_prompts_and_several_tokens(fp8):
     counts = [5, 3, 1, 2, 3, 3, 4, 5, 5, 2, 2, 1, 5, 5, 1, 5, 5, 7]
     cu = np.concatenate([[0], np.cumsum(counts)]).tolist()
     for layer in range(2):
-        check_attention(both, layer, slots, cu, 28, share=True, n_tokens=cu[-1] + 3)
+        check_attention(both, layer, slots, cu, 28, share=2, n_tokens=cu[-1] + 3)
     order = [slots[i] for i in (9, 0, 17, 4, 1, 8, 12)]
-    check_attention(both, 0, order, list(range(len(order) + 1)), 28, share=True)
+    check_attention(both, 0, order, list(range(len(order) + 1)), 28, share=2)
 
 
 @pytest.mark.parametrize("groups,n,prompt", [(1, 2, 40000), (3, 40, 5000), (16, 3, 1100), (40, 2, 600)])
@@ -163,7 +163,7 @@ def test_long_prompts_split_over_blocks(groups, n, prompt):
     """Stretches that begin and end inside chunks of one and two rows of accumulators."""
     heads = (8, 2)
     both, slots = forked(heads, 64, [prompt + 33 * i for i in range(groups)], [[1 + (i * 5 + g) % 20 for i in range(n)] for g in range(groups)], seed=groups)
-    check_attention(both, 0, slots, list(range(len(slots) + 1)), heads[0], share=True)
+    check_attention(both, 0, slots, list(range(len(slots) + 1)), heads[0], share=2)
 
 
 def test_a_shared_prefix_of_any_size_of_logits():
@@ -176,12 +176,12 @@ def test_a_shared_prefix_of_any_size_of_logits():
     both.cache.k.copy_(both.dev(o.k))
     q = torch.randn((4, 4, 128)) * 0.3 + torch.tensor([1.0, -1.0, 0.0, 0.05])[None, :, None]
     q = q.to(torch.bfloat16)
-    check_attention(both, 0, slots, [0, 1, 2, 3, 4], 4, share=True, q=(q.cuda(), q.double().numpy()))
+    check_attention(both, 0, slots, [0, 1, 2, 3, 4], 4, share=2, q=(q.cuda(), q.double().numpy()))
     for pool, value in ((both.cache.k, float("nan")), (both.cache.v, float("nan")), (both.cache.k, float("inf"))):
         keep = pool[0, int(o.table[0, 20]), 0, 3].clone()
         pool[0, int(o.table[0, 20]), 0, 3] = value
         batch = both.cache.batch(ints(slots), ints([0, 1, 2, 3, 4]), n_tokens=4, n_q_heads=4)
-        both.cache.plan(batch)
+        both.cache.plan(batch, share=2)
         # (a key of infinity against queries that are all negative is a logit of -inf: a weight of zero)
         zero_weight = (q.double() * float("inf")).sum(-1).cuda() == float("-inf") if value == float("inf") else torch.zeros((4, 4), dtype=bool, device="cuda")
         assert torch.equal(torch.isnan(both.cache.attend(0, batch, q.cuda())), ~zero_weight[:, :, None].expand(4, 4, 128))
@@ -192,7 +192,29 @@ def test_shared_and_alone_agree_and_repeat():
     both, slots = forked((32, 8), 64, [3000], [[1 + i for i in range(20)]], seed=3)
     q = queries(both.rng, 20, 32)
     _, alone, _ = check_attention(both, 0, slots, list(range(21)), 32, share=False, q=q)
-    _, out, lse = check_attention(both, 0, slots, list(range(21)), 32, share=True, q=q)
+    _, out, lse = check_attention(both, 0, slots, list(range(21)), 32, share=2, q=q)
     for _ in range(3):
-        _, again, lse2 = check_attention(both, 0, slots, list(range(21)), 32, share=True, q=q)
+        _, again, lse2 = check_attention(both, 0, slots, list(range(21)), 32, share=2, q=q)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+def test_a_plan_that_shares_wants_its_prefixes_read():
+    """A plan with shared prefixes and an attention told that nothing is: refused, nothing written."""
+    both, slots = forked((8, 2), 16, [1600], [[3, 4, 5, 6]], seed=1)
+    batch = both.cache.batch(ints(slots), ints([0, 1, 2, 3, 4]), n_tokens=4, n_q_heads=8)
+    out = torch.full((4, 8, 128), 7.0, dtype=torch.bfloat16, device="cuda")
+    both.cache.plan(batch, share=2)
+    batch.share = 0
+    both.cache.attend(0, batch, torch.ones_like(out), out)
+    assert B.asl_pages_status(both.cache.ctx, both.cache.pages) == (B.ASL_ERR_WORKSPACE, -1)
+    assert (out == 7.0).all()
+    for share in (-1, 3):
+        with pytest.raises(B.AslError):
+            both.cache.plan(batch, share=share)
+
+
+def test_sharing_where_it_saves_enough():
+    """share = 1: nothing is told apart by the results, whether the prefix is read once (32 MB or more saved) or by each."""
+    for prompt, n in ((600, 5), (2100, 40)):
+        both, slots = forked((32, 8), 64, [prompt], [[1 + i % 7 for i in range(n)]], seed=n)
+        check_attention(both, 0, slots, list(range(n + 1)), 32, share=1)

@@ -14,7 +14,7 @@ from pages_check import Both, bits, check_attention, ints, queries
 pytestmark = pytest.mark.gpu
 
 
-def step(both, slots, n_q_heads, counts, share=True):
+def step(both, slots, n_q_heads, counts, share=2):
     """One decoding step of `counts` tokens for each slot: grow, append on every layer, attend on every layer."""
     want = [-1] * len(both.oracle.len)
     for s, c in zip(slots, counts):
@@ -98,7 +98,7 @@ def test_a_decoding_step_replayed():
         cache.reserve(want)
         for layer in layers:
             cache.append(layer, batch, k_new[layer], v_new[layer])
-        cache.plan(batch)
+        cache.plan(batch, share=2)
         for layer in layers:
             cache.attend(layer, batch, q[layer], out[layer], lse[layer])
 
@@ -162,7 +162,7 @@ def test_two_caches_on_two_streams():
     for _ in range(8):
         for i, (both, heads, q, slots, cu, batch, stream) in enumerate(work):
             with torch.cuda.stream(stream):
-                both.cache.plan(batch)
+                both.cache.plan(batch, share=2)
                 outs[i].append(both.cache.attend(0, batch, q[0]))
     torch.cuda.synchronize()
     for i, (both, heads, q, slots, cu, batch, stream) in enumerate(work):
@@ -196,7 +196,7 @@ def test_pages_far_into_a_large_pool():
     cache.append(0, one, *tail)
     q = torch.randn((8, 32, 128), generator=g, device="cuda").to(torch.bfloat16)
     assert int(table[0, 0]) >= n_pages - 60
-    cache.plan(one)
+    cache.plan(one, share=2)
     out = cache.attend(0, one, q)
     cache.plan(one, share=False)
     alone = cache.attend(0, one, q)
@@ -222,7 +222,7 @@ def test_as_many_sequences_as_a_batch_has():
     want = [(i % 40) + 1 if i % 2 == 0 else 0 for i in range(n)]
     both.fill(want)
     both.fork([i - 1 if i % 2 else -1 for i in range(n)])
-    check_attention(both, 0, list(range(n)), list(range(n + 1)), 2, share=True)
+    check_attention(both, 0, list(range(n)), list(range(n + 1)), 2, share=2)
 
 
 def test_batches_that_are_not_ascending_are_refused():

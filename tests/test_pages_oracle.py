@@ -114,6 +114,6 @@ def test_calls_that_are_refused():
     assert lib.asl_pages_store(None, C.byref(p), 0, a, a, a, a, None) == B.ASL_ERR_INVALID
     assert lib.asl_pages_compact(None, C.byref(p), 0, a, a, a, 1, a, 1, 1, None) == B.ASL_ERR_INVALID
     assert lib.asl_pages_append(None, C.byref(p), 0, C.byref(batch), a, a, two, two, None) == B.ASL_ERR_INVALID
-    assert lib.asl_attend(None, C.byref(p), 0, C.byref(batch), 8, a, two, a, a, a, 1 << 30, None) == B.ASL_ERR_INVALID
+    assert lib.asl_attend(None, C.byref(p), 0, C.byref(batch), 8, 1, a, two, a, a, a, 1 << 30, None) == B.ASL_ERR_INVALID
     assert lib.asl_pages_status(None, C.byref(p), None, None) == B.ASL_ERR_INVALID
     assert "pages" in B.asl_strerror(B.ASL_ERR_PAGES)
