@@ -48,25 +48,28 @@ __global__ void __launch_bounds__(SAME_THREADS) attend_same_kernel(PagePool g, a
   if (tid == 0) same[i] = m;
 }
 
-__device__ __forceinline__ int scan_step(int v, int* part, int& total) {       // as block_scan, 512 threads
+// exclusive prefix sums of two values per thread over the block; x and y: the sums.  `part`: [2][warps] of shared memory.
+__device__ __forceinline__ int2 scan_step(int2 v, int2* part, int2& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int s = v;
+  int2 s = v;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, s, o);
-    if (lane >= o) s += u;
+    const int x = __shfl_up_sync(0xffffffffu, s.x, o), y = __shfl_up_sync(0xffffffffu, s.y, o);
+    if (lane >= o) { s.x += x; s.y += y; }
   }
   if (lane == 31) part[warp] = s;
   __syncthreads();
-  int before = 0;
-  total = 0;
+  int2 before = {0, 0};
+  total = {0, 0};
 #pragma unroll
   for (int k = 0; k < PLAN_THREADS / 32; ++k) {
-    if (k < warp) before += part[k];
-    total += part[k];
+    const int2 p = part[k];
+    if (k < warp) { before.x += p.x; before.y += p.y; }
+    total.x += p.x;
+    total.y += p.y;
   }
   __syncthreads();
-  return before + s - v;
+  return {before.x + s.x - v.x, before.y + s.y - v.y};
 }
 
 struct PlanArgs {
@@ -79,10 +82,10 @@ struct PlanArgs {
 };
 
 // One block: groups of neighbours, prefix sums over sequences and groups, and where every CTA's stretch begins.  All of it in
-// shared memory: what bounds it is the chain of its steps (two loads, the groups' walk of some 30 clk an entry, four prefix sums).
+// shared memory: what bounds it is the chain of its steps (two loads, the groups' walk entry by entry, three prefix sums).
 __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   extern __shared__ int32_t sm[];
-  __shared__ int part[PLAN_THREADS / 32];
+  __shared__ int2 part[PLAN_THREADS / 32];
   __shared__ int n_groups_s, any_full, bad;
   __shared__ unsigned long long most_s;
   pdl_wait_predecessor();
@@ -102,6 +105,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; bad = 0; }
   for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tokens[t].seq.ntok = 0;
   __syncthreads();
+  unsigned long long most = 0;             // tiles, were nothing shared: they are counted in 32 bits
   for (int i = tid; i < n; i += PLAN_THREADS) {
     const int s = __ldcg(a.b.slots + i), t0 = __ldcg(a.b.cu_q + i), t1 = __ldcg(a.b.cu_q + i + 1);
     const int same = a.share == 1 ? __ldcg(a.w.same + i) : 0;
@@ -114,9 +118,11 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     tok0[i] = t0;
     len[i] = m ? min(max(l, 0), a.g.max_pages << a.g.page_shift) : 0;
     com[i] = same << a.g.page_shift;
-    // tiles, were nothing shared: they are counted in 32 bits
-    if (m) atomicAdd(&most_s, (unsigned long long)narrow_chunks_of(m, G) * (unsigned)(len[i] / NARROW_KEYS + 2));
+    if (m) most += (unsigned long long)narrow_chunks_of(m, G) * (unsigned)(len[i] / NARROW_KEYS + 2);
   }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) most += __shfl_xor_sync(0xffffffffu, most, o);
+  if ((tid & 31) == 0 && most) atomicAdd(&most_s, most);
   __syncthreads();
   if (bad || most_s * H >= 1ull << 30) {
     if (tid == 0) note_error(a.g.err, bad ? ASL_ERR_INVALID : ASL_ERR_UNSUPPORTED, -1);
@@ -153,15 +159,16 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   __syncthreads();
   if (tid == 0) {
     int ng = 0, held = 0, keys = 0;                          // of the open group: entries (0: none is open), shared tokens
-    float saved = 0.0f;                                      // keys read less often, by all groups so far
+    int64_t saved = 0;                                       // keys read less often, by all groups so far
     int has = ntok[0], mine = own[0], with = com[0];
     for (int i = 0; i < n; ++i) {
       const int j = min(i + 1, n - 1), has2 = ntok[j], mine2 = own[j], with2 = com[j];       // (ahead of this entry's stores)
       const int both = min(keys, with);
-      const bool joins = has && held && both > 0 && (float)held * both >= (float)(held - 1) * keys;
+      const int64_t before = (int64_t)(held - 1) * keys;     // saved by the open group
+      const bool joins = has && held && both > 0 && (int64_t)held * both >= before;
       if (!joins && held) {
         gpfx[ng - 1] = held > 1 ? keys : 0;
-        saved += (float)(held - 1) * keys;
+        saved += before;
       }
       if (!joins && has) gat[ng++] = i;
       held = has ? (joins ? held + 1 : 1) : 0;
@@ -171,9 +178,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     }
     if (held) {
       gpfx[ng - 1] = held > 1 ? keys : 0;
-      saved += (float)(held - 1) * keys;
+      saved += (int64_t)(held - 1) * keys;
     }
-    if (saved * H * (a.g.k_row + a.g.v_row) < a.min_bytes)
+    if ((float)saved * H * (a.g.k_row + a.g.v_row) < a.min_bytes)
       for (int g = 0; g < ng; ++g) gpfx[g] = 0;
     n_groups_s = ng;
   }
@@ -188,15 +195,16 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       nc = narrow_chunks_of(ntok[i], G);
       nt = nc * max(1, (len[i] - pfx + NARROW_KEYS - 1) / NARROW_KEYS);
     }
-    int tsum, csum;
-    const int t0 = tiles + scan_step(nt, part, tsum), c0 = chunks + scan_step(nc, part, csum);
+    int2 sum;
+    const int2 at = scan_step({nt, nc}, part, sum);
+    const int t0 = tiles + at.x, c0 = chunks + at.y;
     if (i < n) {
       first[i] = t0;
       com[i] = c0;
       a.w.seqs[i] = {tok0[i], ntok[i], slot[i], len[i], pfx, t0, c0, grp[i]};
     }
-    tiles += tsum;
-    chunks += csum;
+    tiles += sum.x;
+    chunks += sum.y;
   }
   // groups: their cost, from it what a CTA has of it and the stripes, then the chunks of stripes
   int cost = 0, wchunks = 0;
@@ -212,10 +220,10 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
       c = w.tiles * w.sum;
       if (gpfx[i] && gtok[i] * G > WIDE_ROWS / 2) any_full = 1;
     }
-    int csum;
-    const int c0 = cost + scan_step(c, part, csum);
+    int2 sum;
+    const int c0 = cost + scan_step({c, 0}, part, sum).x;
     if (i < ng) gcost[i] = c0;
-    cost += csum;
+    cost += sum.x;
   }
   if (tid == 0) { first[n] = tiles; gcost[ng] = cost; }
   __syncthreads();
@@ -232,13 +240,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
         const WideShape w(gtok[i], gpfx[i], G, stripe);
         nc = w.chunks * w.stripes;
       }
-      int nsum;
-      const int n0 = wchunks + scan_step(nc, part, nsum);
+      int2 sum;
+      const int n0 = wchunks + scan_step({nc, 0}, part, sum).x;
       if (i < ng) {
         gchunk[i] = n0;
         a.w.groups[i] = group_of(i);
       }
-      wchunks += nsum;
+      wchunks += sum.x;
     }
   }
   __syncthreads();
