@@ -364,6 +364,7 @@ typedef struct {
   int32_t max_seqs;       /* slots, at most 65536                                                */
   int32_t max_pages;      /* length of a slot's row of the table; max_pages * page_size < 2^31   */
   int32_t k_dtype;        /* ASL_K_BF16, or ASL_K_FP8_E4M3: K holds codes, the key is code x k_scale[layer][kv head] */
+                          /* (the NaN codes are read as 480, the value that their bits would have)  */
   void* k;                /* device [n_layers][n_pages][H_k][page_size][d], bf16 or E4M3 codes, 16-byte aligned */
   void* v;                /* device, the same in bf16                                            */
   const float* k_scale;   /* device [n_layers][H_k], finite and > 0; read only for ASL_K_FP8_E4M3 */

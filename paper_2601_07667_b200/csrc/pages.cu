@@ -9,6 +9,10 @@
 namespace {
 
 constexpr int TABLE_THREADS = 1024;
+// Bytes of K and V up to which copies on write are left to the block that keeps the books: a launch costs the host 2 us and the device
+// one or two (four children of a prompt of 519 tokens: a round 13.4 -> 12.5 us on the device, 22.5 -> 20.5 from the host; a unit
+// at a time by the whole block it took 19).
+constexpr int64_t COPY_INSIDE = 256 * 1024;
 constexpr int SCRATCH_HEAD = 4;           // words: copies on write of the latest reserve, unused x 3
 // scratch: head, {old page, new page, tokens, unused} of each copy [max_seqs], offsets in the list of free pages [max_seqs], that list [n_pages]
 
@@ -39,8 +43,42 @@ __device__ __forceinline__ int block_scan(int v, int* part, int& total) {
   return before;
 }
 
+// The tokens held of shared last pages, in all layers: a unit is (copy, layer, kv head), its rows lie together.  Units first, first
+// + step ... by `threads` threads, of which this is number `me`.
+__device__ __forceinline__ void copy_units(const PagePool& g, int n_layers, const int4* cow, int n, int first, int step, int me, int threads) {
+  const int64_t units = (int64_t)n * n_layers * g.n_kv_heads;
+  const int64_t rows = (int64_t)g.n_pages * g.n_kv_heads << g.page_shift;
+  for (int64_t u = first; u < units; u += step) {
+    const int h = (int)(u % g.n_kv_heads), l = (int)(u / g.n_kv_heads % n_layers);
+    const int4 c = cow[u / g.n_kv_heads / n_layers];
+    const int64_t from = ((int64_t)c.x * g.n_kv_heads + h) << g.page_shift, to = ((int64_t)c.y * g.n_kv_heads + h) << g.page_shift;
+    const uint4* ks = reinterpret_cast<const uint4*>(g.k + (l * rows + from) * g.k_row);
+    const uint4* vs = reinterpret_cast<const uint4*>(g.v + (l * rows + from) * g.v_row);
+    uint4* kd = reinterpret_cast<uint4*>(g.k + (l * rows + to) * g.k_row);
+    uint4* vd = reinterpret_cast<uint4*>(g.v + (l * rows + to) * g.v_row);
+    const int nk = c.z * g.k_row / 16, nv = c.z * g.v_row / 16;       // at most 128 rows of 16 vectors
+    for (int i0 = me; i0 < nv; i0 += 4 * threads) {
+      uint4 a[4], b[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (i0 + threads * q < nk) a[q] = __ldcg(ks + i0 + threads * q);
+        if (i0 + threads * q < nv) b[q] = __ldcg(vs + i0 + threads * q);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (i0 + threads * q < nk) kd[i0 + threads * q] = a[q];
+        if (i0 + threads * q < nv) vd[i0 + threads * q] = b[q];
+      }
+    }
+  }
+}
+__global__ void __launch_bounds__(256) pages_copy_kernel(PagePool g, int n_layers, const int32_t* scratch) {
+  pdl_wait_predecessor();
+  copy_units(g, n_layers, reinterpret_cast<const int4*>(scratch + SCRATCH_HEAD), *scratch, blockIdx.x, gridDim.x, threadIdx.x, 256);
+}
+
 // One block: the free pages as a bitmap in shared memory, the slots' needs and their prefix sums, then the pages.
-__global__ void __launch_bounds__(TABLE_THREADS) pages_reserve_kernel(PagePool g, const int32_t* __restrict__ want, int32_t* scratch) {
+__global__ void __launch_bounds__(TABLE_THREADS) pages_reserve_kernel(PagePool g, const int32_t* __restrict__ want, int32_t* scratch, int copy_layers) {
   extern __shared__ uint32_t bits[];       // one bit per page: free
   __shared__ int part[33];
   __shared__ int bad;
@@ -158,38 +196,9 @@ __global__ void __launch_bounds__(TABLE_THREADS) pages_reserve_kernel(PagePool g
       }
     }
   }
-}
-
-// The tokens held of shared last pages, in all layers: a unit is (copy, layer, kv head), its rows lie together.
-__global__ void __launch_bounds__(256) pages_copy_kernel(PagePool g, int n_layers, const int32_t* __restrict__ scratch) {
-  pdl_wait_predecessor();
-  const int n = __ldcg(scratch);
-  const int4* cow = reinterpret_cast<const int4*>(scratch + SCRATCH_HEAD);
-  const int64_t units = (int64_t)n * n_layers * g.n_kv_heads;
-  const int64_t pages_bytes_k = ((int64_t)g.n_pages * g.n_kv_heads << g.page_shift) * g.k_row;
-  const int64_t pages_bytes_v = ((int64_t)g.n_pages * g.n_kv_heads << g.page_shift) * g.v_row;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int h = (int)(u % g.n_kv_heads), l = (int)(u / g.n_kv_heads % n_layers);
-    const int4 c = __ldcg(cow + u / g.n_kv_heads / n_layers);
-    const int64_t from = ((int64_t)c.x * g.n_kv_heads + h) << g.page_shift, to = ((int64_t)c.y * g.n_kv_heads + h) << g.page_shift;
-    const uint4* ks = reinterpret_cast<const uint4*>(g.k + l * pages_bytes_k + from * g.k_row);
-    const uint4* vs = reinterpret_cast<const uint4*>(g.v + l * pages_bytes_v + from * g.v_row);
-    uint4* kd = reinterpret_cast<uint4*>(g.k + l * pages_bytes_k + to * g.k_row);
-    uint4* vd = reinterpret_cast<uint4*>(g.v + l * pages_bytes_v + to * g.v_row);
-    const int nk = c.z * g.k_row / 16, nv = c.z * g.v_row / 16;       // at most 128 rows of 16 vectors
-    for (int i0 = threadIdx.x; i0 < nv; i0 += 1024) {
-      uint4 a[4], b[4];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (i0 + 256 * q < nk) a[q] = __ldcg(ks + i0 + 256 * q);
-        if (i0 + 256 * q < nv) b[q] = __ldcg(vs + i0 + 256 * q);
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (i0 + 256 * q < nk) kd[i0 + 256 * q] = a[q];
-        if (i0 + 256 * q < nv) vd[i0 + 256 * q] = b[q];
-      }
-    }
+  if (copy_layers) {                       // few copies at most: no launch of their own
+    __syncthreads();
+    copy_units(g, copy_layers, cow, scratch[0], tid / 128, TABLE_THREADS / 128, tid % 128, 128);
   }
 }
 
@@ -426,9 +435,12 @@ asl_status asl_pages_reserve(asl_ctx* c, const asl_pages* p, const int32_t* want
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t smem = ((size_t)p->n_pages + 31) / 32 * 4;
   if (smem > 48 * 1024) ASL_CUDA(cudaFuncSetAttribute(pages_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 1 << 17));
-  launch_after_smem(pages_reserve_kernel, dim3(1), dim3(TABLE_THREADS), smem, st, page_pool(p, 0), want, p->scratch);
-  launch_after(pages_copy_kernel, dim3(c->sm_count * 8), dim3(256), st, page_pool(p, 0), p->n_layers, static_cast<const int32_t*>(p->scratch));
-  return launched(c, 2);
+  const int64_t most = (int64_t)p->max_seqs * p->n_layers * p->n_kv_heads * p->page_size * p->head_dim * 4;      // bytes copied at most
+  const bool inside = most <= COPY_INSIDE;
+  launch_after_smem(pages_reserve_kernel, dim3(1), dim3(TABLE_THREADS), smem, st, page_pool(p, 0), want, p->scratch, inside ? p->n_layers : 0);
+  if (!inside)
+    launch_after(pages_copy_kernel, dim3(c->sm_count * 8), dim3(256), st, page_pool(p, 0), p->n_layers, static_cast<const int32_t*>(p->scratch));
+  return launched(c, inside ? 1 : 2);
 }
 
 asl_status asl_pages_fork(asl_ctx* c, const asl_pages* p, const int32_t* parent, void* stream) {
