@@ -444,8 +444,9 @@ asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, 
  * looks for neighbours of the batch whose pages begin alike (forks of one prompt, side by side) and, where that saves
  * enough, such a prefix is read once for all of them, their rows multiplied together; with 2 wherever a page is
  * shared; with 0 every sequence reads its own.  asl_attend is given the plan's `share`; its kernels follow one another on
- * the stream, so that no other thread may launch on it meanwhile.  The workspace (asl_attend_workspace bytes, 256-byte aligned) carries the plan and the parts of rows
- * whose keys are split over several blocks; calls that share it have to be ordered one behind another.
+ * the stream, so that no other thread may launch on it meanwhile.  The workspace (asl_attend_workspace bytes, 256-byte
+ * aligned) carries the plan and the parts of rows whose keys are split over several blocks; calls that share it have to be
+ * ordered one behind another.
  * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its sizes writes nothing
  * and notes ASL_ERR_WORKSPACE; after an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
 asl_status asl_attend_workspace(const asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, size_t* bytes);

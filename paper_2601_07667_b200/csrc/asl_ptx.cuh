@@ -212,11 +212,6 @@ __device__ __forceinline__ void tc_ld_wait(uint32_t (&r)[16]) {
                : "memory");
 }
 // Registers into consecutive columns of this thread's lane; tc_st_wait before anyone reads them.
-__device__ __forceinline__ void tc_st_lane8(uint32_t taddr, const uint32_t (&r)[8]) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
 __device__ __forceinline__ void tc_st_lane(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "

@@ -18,7 +18,7 @@ constexpr int ATTEND_MAX_SEQS = 4096;
 
 struct __align__(16) AttendHead {        // one per plan, on the device
   int32_t mark, n_seqs, n_tokens, n_q_heads;          // what the layout follows from: see plan_fits
-  int32_t n_kv_heads, n_groups, narrow_tiles, narrow_chunks;   // tiles and chunks per kv head
+  int32_t n_kv_heads, pad0, narrow_tiles, narrow_chunks;       // tiles and chunks per kv head
   int32_t narrow_each, wide_cost, wide_chunks, wide_each;      // tiles and cost per CTA; cost and chunks per kv head
 };
 constexpr int ATTEND_MARK = 0x41534c50;
@@ -73,11 +73,7 @@ struct AttendArgs {
 };
 
 // Tokens of a chunk of a group's rows (at least two, since a token has at most 128).
-#ifdef __CUDACC__
-__host__
-__device__
-#endif
-inline int wide_tokens(int G) { return WIDE_ROWS / G; }
+ASL_HD inline int wide_tokens(int G) { return WIDE_ROWS / G; }
 
 #ifdef __CUDACC__
 // Every warp reads the head: by loads that L1 keeps (written two launches ago or more), since thousands of requests for one

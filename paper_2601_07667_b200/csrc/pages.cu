@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(TABLE_THREADS) pages_reserve_kernel(PagePool g
   }
   if (copy_layers) {                       // few copies at most: no launch of their own
     __syncthreads();
-    copy_units(g, copy_layers, cow, scratch[0], tid / 128, TABLE_THREADS / 128, tid % 128, 128);
+    copy_units(g, copy_layers, cow, __ldcg(scratch), tid / 128, TABLE_THREADS / 128, tid % 128, 128);
   }
 }
 
