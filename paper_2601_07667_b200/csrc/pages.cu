@@ -434,7 +434,10 @@ asl_status asl_pages_reserve(asl_ctx* c, const asl_pages* p, const int32_t* want
   if (!p->scratch || p->scratch_bytes < scratch_bytes_of(p) || !asl_aligned16(p->scratch)) return ASL_ERR_WORKSPACE;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const size_t smem = ((size_t)p->n_pages + 31) / 32 * 4;
-  if (smem > 48 * 1024) ASL_CUDA(cudaFuncSetAttribute(pages_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 1 << 17));
+  if (!c->reserve_ready) {                 // (whatever the pool: the 48 KB that need no leave hold the kernel's own arrays too)
+    ASL_CUDA(cudaFuncSetAttribute(pages_reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 1 << 17));
+    c->reserve_ready = true;
+  }
   const int64_t most = (int64_t)p->max_seqs * p->n_layers * p->n_kv_heads * p->page_size * p->head_dim * 4;      // bytes copied at most
   const bool inside = most <= COPY_INSIDE;
   launch_after_smem(pages_reserve_kernel, dim3(1), dim3(TABLE_THREADS), smem, st, page_pool(p, 0), want, p->scratch, inside ? p->n_layers : 0);

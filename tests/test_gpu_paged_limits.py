@@ -1,0 +1,30 @@
+"""The paged cache at sizes around what a kernel's shared memory holds by default."""
+import pytest
+import torch
+
+from paper_2601_07667_b200 import binding as B
+
+from pages_check import ints
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n_pages", [392064, 392065, 392500, 393216, 393217])
+def test_a_pool_whose_books_are_about_48_kb(n_pages):
+    """Each pool on a context of its own: slots grow over what is free, with a copy of a shared last page."""
+    k = torch.zeros((1, n_pages, 1, 16, 128), dtype=torch.uint8, device="cuda")
+    v = torch.zeros((1, n_pages, 1, 16, 128), dtype=torch.bfloat16, device="cuda")
+    table, length = torch.zeros((3, 64), dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    refs = torch.ones(n_pages, dtype=torch.int32, device="cuda")
+    free = [5, 70000, 392000, 392063, n_pages - 2, n_pages - 1]
+    free = sorted(set(free))
+    refs[torch.tensor(free, device="cuda")] = 0
+    cache = B.PagedCache(page_size=16, k=k, v=v, table=table, length=length, refs=refs, k_scale=torch.ones((1, 1)))
+    cache.reserve(ints([20, -1, -1]))
+    cache.fork(ints([-1, 0, -1]))
+    cache.reserve(ints([-1, 21, -1]))
+    cache.check()
+    assert length.tolist() == [20, 21, 0]
+    assert table[0, :2].tolist() == free[:2] and table[1, :2].tolist() == [free[0], free[2]]
+    assert [int(refs[p]) for p in free[:4]] == [2, 1, 1, 0]
+    cache.close()

@@ -1,0 +1,72 @@
+"""What the paged cache's entry points launch, checked on the CPU: their built objects linked against a runtime that only logs
+launches and refuses those that the real one would (fake_launches.cpp)."""
+import ctypes as C
+import os
+import subprocess
+
+import pytest
+
+from paper_2601_07667_b200 import binding as B
+from paper_2601_07667_b200 import build
+
+from test_layer_order import CUDA_INCLUDE
+
+A = 0x1000                                              # an address that is never looked at
+NAMES = [n for n in B.EXPORTS if n.startswith(("asl_pages_", "asl_attend"))] + ["asl_create", "asl_destroy"]
+
+
+@pytest.fixture(scope="module")
+def built(tmp_path_factory):
+    build.build()
+    objects = [os.path.join(build.OBJ_DIR, n) for n in ("pages.o", "attend.o")]
+    if not all(os.path.exists(o) for o in objects):
+        build.build(force=True)
+    so = str(tmp_path_factory.mktemp("fake") / "libasl_launches.so")
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.run(["g++", "-shared", "-fPIC", "-O1", "-std=c++17", "-Wl,-Bsymbolic", "-I", CUDA_INCLUDE, "-I", build.INCLUDE, "-I", build.CSRC, "-I", here,
+                    "-x", "c++", os.path.join(build.CSRC, "asl_api.cu"), os.path.join(here, "fake_launches.cpp"), "-x", "none", *objects, "-o", so],
+                   check=True)
+    return so
+
+
+@pytest.fixture
+def lib(built, tmp_path):
+    """A copy of its own, so that no attribute of a kernel is left from another test."""
+    so = str(tmp_path / "lib.so")
+    with open(built, "rb") as f, open(so, "wb") as g:
+        g.write(f.read())
+    fake = C.CDLL(so)
+    fake.fake_log.restype = C.c_char_p
+    for name in NAMES:
+        getattr(fake, name).argtypes = getattr(B.library(), name).argtypes
+    fake.fake_fail(b"", 0)
+    return fake
+
+
+class Cache:
+    def __init__(self, lib, **sizes):
+        self.lib, self.ctx = lib, C.c_void_p()
+        assert lib.asl_create(C.byref(self.ctx), 0) == B.ASL_OK
+        s = dict(n_layers=2, n_kv_heads=2, page_size=16, n_pages=100, max_seqs=8, max_pages=16, k_dtype=B.ASL_K_BF16)
+        s.update(sizes)
+        self.pages = B.AslPages(s["n_layers"], s["n_kv_heads"], 128, s["page_size"], s["n_pages"], s["max_seqs"], s["max_pages"], s["k_dtype"],
+                                A, A, A, A, A, A, A, A, 1 << 40)
+        self.ref = C.byref(self.pages)
+        lib.fake_clear()
+
+    def launches(self):
+        """(kernel, grid, block, dynamic bytes) of every launch since the latest look."""
+        got = [l.split() for l in self.lib.fake_log().decode().splitlines()]
+        self.lib.fake_clear()
+        return [(x[0], *map(int, x[1:])) if x[0] != "run" else tuple(x[1:2]) for x in got]
+
+    def kernels(self):
+        return [x[0] for x in self.launches()]
+
+
+@pytest.mark.parametrize("n_pages", [1, 70001, 392063, 392064, 392065, 392500, 393216, 393217, 1 << 20])
+def test_the_books_of_a_pool_of_any_size(lib, n_pages):
+    """A bit a page lies in shared memory beside the kernel's own arrays: up to 48 KB together need no leave, more do."""
+    c = Cache(lib, n_pages=n_pages, n_layers=64, max_seqs=64)
+    assert lib.asl_pages_reserve(c.ctx, c.ref, A, None) == B.ASL_OK
+    assert c.kernels() == ["pages_reserve_kernel", "pages_copy_kernel"]
