@@ -383,8 +383,8 @@ size_t scratch_bytes_of(const asl_pages* p) {
 }
 
 asl_status launched(asl_ctx* c, int n) {
-  c->launches += n;
   ASL_CUDA(cudaGetLastError());
+  c->launches += n;
   return ASL_OK;
 }
 
@@ -441,9 +441,10 @@ asl_status asl_pages_reserve(asl_ctx* c, const asl_pages* p, const int32_t* want
   const int64_t most = (int64_t)p->max_seqs * p->n_layers * p->n_kv_heads * p->page_size * p->head_dim * 4;      // bytes copied at most
   const bool inside = most <= COPY_INSIDE;
   launch_after_smem(pages_reserve_kernel, dim3(1), dim3(TABLE_THREADS), smem, st, page_pool(p, 0), want, p->scratch, inside ? p->n_layers : 0);
-  if (!inside)
-    launch_after(pages_copy_kernel, dim3(c->sm_count * 8), dim3(256), st, page_pool(p, 0), p->n_layers, static_cast<const int32_t*>(p->scratch));
-  return launched(c, inside ? 1 : 2);
+  const asl_status r = launched(c, 1);           // (without the books there is no list of copies)
+  if (r != ASL_OK || inside) return r;
+  launch_after(pages_copy_kernel, dim3(c->sm_count * 8), dim3(256), st, page_pool(p, 0), p->n_layers, static_cast<const int32_t*>(p->scratch));
+  return launched(c, 1);
 }
 
 asl_status asl_pages_fork(asl_ctx* c, const asl_pages* p, const int32_t* parent, void* stream) {

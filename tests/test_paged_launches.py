@@ -70,3 +70,13 @@ def test_the_books_of_a_pool_of_any_size(lib, n_pages):
     c = Cache(lib, n_pages=n_pages, n_layers=64, max_seqs=64)
     assert lib.asl_pages_reserve(c.ctx, c.ref, A, None) == B.ASL_OK
     assert c.kernels() == ["pages_reserve_kernel", "pages_copy_kernel"]
+
+
+def test_no_copies_behind_books_that_were_not_kept(lib):
+    """The copying kernel reads a list that the books' kernel writes: where that one cannot be launched nothing follows it."""
+    c = Cache(lib, n_layers=64, max_seqs=64)
+    lib.fake_fail(b"pages_reserve_kernel", 1)
+    assert lib.asl_pages_reserve(c.ctx, c.ref, A, None) == B.ASL_ERR_CUDA
+    assert c.kernels() == []
+    assert lib.asl_pages_reserve(c.ctx, c.ref, A, None) == B.ASL_OK
+    assert c.kernels() == ["pages_reserve_kernel", "pages_copy_kernel"]
