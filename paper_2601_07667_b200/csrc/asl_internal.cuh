@@ -65,6 +65,7 @@ struct asl_ctx {
   int64_t launches = 0;
   bool attend_ready = false;          // the attention kernels have been given their shared memory on the context's device
   bool reserve_ready = false;         // and so has the kernel that keeps the pages' books
+  bool plan_ready = false;            // and the one that plans
   // asl_run_layer: order between a layer's streams, and when the buffers of a slot are free again
   cudaEvent_t ev_scored = nullptr, ev_pooled = nullptr, ev_done[2][2] = {};
   bool pending[2] = {false, false};   // the slot's ev_done have been recorded since asl_run_reset

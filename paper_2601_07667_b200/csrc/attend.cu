@@ -511,8 +511,10 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   a.wide_grid = l.wide_grid;
   a.min_bytes = share == 2 ? 0.0f : SHARE_MIN_BYTES;
   const size_t smem = sizeof(int32_t) * (12 * (size_t)b->n_seqs + 2);
-  if (smem > 48 * 1024)
+  if (!c->plan_ready) {                    // (whatever the batch: the 48 KB that need no leave hold the kernel's own arrays too)
     ASL_CUDA(cudaFuncSetAttribute(attend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 4 * (12 * ATTEND_MAX_SEQS + 2)));
+    c->plan_ready = true;
+  }
   if (a.share == 1) {
     launch_after(attend_same_kernel, dim3(b->n_seqs), dim3(SAME_THREADS), st, a.g, a.b, a.w.same);
     c->launches += 1;

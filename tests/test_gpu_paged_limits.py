@@ -4,7 +4,7 @@ import torch
 
 from paper_2601_07667_b200 import binding as B
 
-from pages_check import ints
+from pages_check import Both, check_attention, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,13 @@ def test_a_pool_whose_books_are_about_48_kb(n_pages):
     assert table[0, :2].tolist() == free[:2] and table[1, :2].tolist() == [free[0], free[2]]
     assert [int(refs[p]) for p in free[:4]] == [2, 1, 1, 0]
     cache.close()
+
+
+@pytest.mark.parametrize("n", [1019, 1020, 1021, 1022, 1023, 1024, 1025])
+def test_a_batch_whose_plan_is_about_48_kb(n):
+    """Each batch on a context of its own; every third sequence a fork of the one before it, one free slot."""
+    both = Both(kv_heads=1, page=16, n_pages=2 * n, max_seqs=n, max_pages=3, seed=n)
+    both.fill([(i % 40) + 1 if i % 3 and i != 7 else 0 for i in range(n)])
+    both.fork([i - 1 if i % 3 == 0 and i else -1 for i in range(n)])
+    check_attention(both, 0, list(range(n)), list(range(n + 1)), 2, share=2)
+    both.cache.close()

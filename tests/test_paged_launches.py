@@ -54,6 +54,15 @@ class Cache:
         self.ref = C.byref(self.pages)
         lib.fake_clear()
 
+    def batch(self, n_seqs, n_tokens, n_q_heads=4):
+        self.b, size = B.AslBatch(n_seqs, n_tokens, A, A), C.c_size_t()
+        assert self.lib.asl_attend_workspace(self.ctx, self.ref, C.byref(self.b), n_q_heads, C.byref(size)) == B.ASL_OK
+        return C.byref(self.b), n_q_heads, size.value
+
+    def plan(self, batch, share=1):
+        b, heads, size = batch
+        return self.lib.asl_attend_plan(self.ctx, self.ref, b, heads, share, A, size, None)
+
     def launches(self):
         """(kernel, grid, block, dynamic bytes) of every launch since the latest look."""
         got = [l.split() for l in self.lib.fake_log().decode().splitlines()]
@@ -80,3 +89,11 @@ def test_no_copies_behind_books_that_were_not_kept(lib):
     assert c.kernels() == []
     assert lib.asl_pages_reserve(c.ctx, c.ref, A, None) == B.ASL_OK
     assert c.kernels() == ["pages_reserve_kernel", "pages_copy_kernel"]
+
+
+@pytest.mark.parametrize("n_seqs", [1, 1000, 1019, 1020, 1021, 1022, 1023, 1024, 1025, 4096])
+def test_a_plan_of_any_batch(lib, n_seqs):
+    """Twelve words a sequence in shared memory beside the kernel's own arrays."""
+    c = Cache(lib, max_seqs=4096, max_pages=4)
+    assert c.plan(c.batch(n_seqs, n_seqs)) == B.ASL_OK
+    assert c.kernels() == ["attend_plan_kernel"]
