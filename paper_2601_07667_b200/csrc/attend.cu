@@ -517,11 +517,12 @@ asl_status asl_attend_plan(asl_ctx* c, const asl_pages* p, const asl_batch* b, i
   }
   if (a.share == 1) {
     launch_after(attend_same_kernel, dim3(b->n_seqs), dim3(SAME_THREADS), st, a.g, a.b, a.w.same);
+    ASL_CUDA(cudaGetLastError());          // (the plan reads what it has counted)
     c->launches += 1;
   }
   launch_after_smem(attend_plan_kernel, dim3(1), dim3(PLAN_THREADS), smem, st, a);
-  c->launches += 1;
   ASL_CUDA(cudaGetLastError());
+  c->launches += 1;
   return ASL_OK;
 }
 

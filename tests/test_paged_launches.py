@@ -97,3 +97,14 @@ def test_a_plan_of_any_batch(lib, n_seqs):
     c = Cache(lib, max_seqs=4096, max_pages=4)
     assert c.plan(c.batch(n_seqs, n_seqs)) == B.ASL_OK
     assert c.kernels() == ["attend_plan_kernel"]
+
+
+def test_no_plan_from_pages_that_were_not_compared(lib):
+    """Many pages are compared by a kernel of its own: where that one cannot be launched the plan does not read its counts."""
+    c = Cache(lib, max_seqs=64, max_pages=1 << 14)
+    batch = c.batch(64, 64)
+    lib.fake_fail(b"attend_same_kernel", 1)
+    assert c.plan(batch) == B.ASL_ERR_CUDA
+    assert c.kernels() == []
+    assert c.plan(batch) == B.ASL_OK
+    assert c.kernels() == ["attend_same_kernel", "attend_plan_kernel"]
