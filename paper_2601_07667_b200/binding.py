@@ -575,7 +575,7 @@ class PagedCache:
             length = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
             refs = torch.zeros(n_pages, dtype=torch.int32, device=dev)
         self.dev, self.ctx = k.device, 0
-        self._i32, self._device, self._strides = torch.int32, k.get_device(), {}
+        self._look_at(k, table)
         if k.dim() != 5 or v.shape != k.shape or k.shape[3] != page_size or v.dtype != torch.bfloat16 or table.dim() != 2:
             raise AslError(ASL_ERR_INVALID, "PagedCache: k and v are [n_layers][n_pages][H_k][page_size][d]")
         if k.element_size() == 1:
@@ -602,8 +602,14 @@ class PagedCache:
         self.pages.scratch_bytes = asl_pages_scratch(self.pages)
         self.scratch = torch.empty(self.pages.scratch_bytes, dtype=torch.uint8, device=self.dev)
         self.pages.scratch = _ptr(self.scratch)
-        self._ref, self._slots, self._d, self._k_bytes = C.byref(self.pages), table.shape[0], k.shape[4], k.element_size()
+        self._ref = C.byref(self.pages)
         self.ctx = asl_create(self._device)
+
+    def _look_at(self, k, table) -> None:
+        """What the calls' checks compare their arguments with."""
+        torch = self.torch
+        self._i32, self._bf16, self._f32 = torch.int32, torch.bfloat16, torch.float32
+        self._device, self._strides, self._slots, self._d, self._k_type = k.get_device(), {}, table.shape[0], k.shape[-1], k.dtype
 
     def _ints(self, x, what: str):
         if x.dtype is not self._i32 or not x.is_contiguous() or x.get_device() != self._device:
@@ -615,11 +621,11 @@ class PagedCache:
             raise AslError(ASL_ERR_INVALID, f"{what}: one value per slot")
         return self._ints(x, what).data_ptr()
 
-    def _rows(self, x, what: str, n_tokens: int, heads: int, bytes_: int = 2):
+    def _rows(self, x, what: str, n_tokens: int, heads: int, codes: bool = False):
         """A [tokens][heads][d] tensor's strides."""
         if x.dim() != 3 or x.shape[0] < n_tokens or x.shape[1] != heads or x.shape[2] != self._d or x.stride(2) != 1:
             raise AslError(ASL_ERR_INVALID, f"{what}: [tokens][heads][d] with dense rows")
-        if x.element_size() != bytes_ or x.get_device() != self._device:
+        if (x.element_size() != 1 if codes else x.dtype is not self._bf16) or x.get_device() != self._device:
             raise AslError(ASL_ERR_INVALID, f"{what}: element type or device")
         key = (x.stride(0), x.stride(1))
         got = self._strides.get(key)
@@ -662,7 +668,7 @@ class PagedCache:
 
     def append(self, layer: int, batch: Batch, k_new, v_new) -> None:
         """K and V rows [n_tokens][H_k][d] of the batch's tokens, to the ends of their sequences."""
-        ks = self._rows(k_new, "k_new", batch.n_tokens, self.pages.n_kv_heads, self._k_bytes)
+        ks = self._rows(k_new, "k_new", batch.n_tokens, self.pages.n_kv_heads, self._k_type is not self._bf16)
         vs = self._rows(v_new, "v_new", batch.n_tokens, self.pages.n_kv_heads)
         _check(_lib.asl_pages_append(self.ctx, self._ref, layer, batch.ref, k_new.data_ptr(), v_new.data_ptr(), ks, vs,
                                      _current_stream()), "asl_pages_append")
@@ -681,9 +687,9 @@ class PagedCache:
         strides = self._rows(q, "q", n, heads)
         if out is None:
             out = self.torch.empty((n, heads, self._d), dtype=q.dtype, device=self.dev)
-        elif not out.is_contiguous() or out.numel() < n * heads * self._d or out.element_size() != 2 or out.get_device() != self._device:
+        elif not out.is_contiguous() or out.numel() < n * heads * self._d or out.dtype is not self._bf16 or out.get_device() != self._device:
             raise AslError(ASL_ERR_INVALID, "out: dense [n_tokens][H_q][d] bf16")
-        if lse is not None and (not lse.is_contiguous() or lse.numel() < n * heads or lse.element_size() != 4 or lse.get_device() != self._device):
+        if lse is not None and (not lse.is_contiguous() or lse.numel() < n * heads or lse.dtype is not self._f32 or lse.get_device() != self._device):
             raise AslError(ASL_ERR_INVALID, "lse: dense [n_tokens][H_q] fp32")
         _check(_lib.asl_attend(self.ctx, self._ref, layer, batch.ref, heads, batch.share, q.data_ptr(), strides, out.data_ptr(),
                                0 if lse is None else lse.data_ptr(), batch.ws, batch.ws_bytes, _current_stream()), "asl_attend")

@@ -1,0 +1,45 @@
+"""Arguments that the paged cache's Python calls refuse, checked on the CPU: the checks look at types, shapes and devices before
+anything is called.  (A cache without a device: only what the checks look at.)"""
+import pytest
+import torch
+
+from paper_2601_07667_b200 import binding as B
+
+
+def bare(codes=False):
+    c = object.__new__(B.PagedCache)
+    c.torch, c.dev, c.ctx = torch, torch.device("cpu"), 0
+    k = torch.zeros((1, 4, 2, 16, 128), dtype=torch.uint8 if codes else torch.bfloat16)
+    c._look_at(k, torch.zeros((3, 4), dtype=torch.int32))
+    c.pages = B.AslPages(1, 2, 128, 16, 4, 3, 4, int(codes), None, None, None, None, None, None, None, None, 0)
+    return c
+
+
+def a_batch(n_tokens=2, n_q_heads=4):
+    b = object.__new__(B.Batch)
+    b.n_tokens, b.n_q_heads, b.share, b.ws, b.ws_bytes, b.ref = n_tokens, n_q_heads, 1, 0, 0, None
+    return b
+
+
+def refused(call):
+    with pytest.raises(B.AslError) as e:
+        call()
+    assert e.value.status == B.ASL_ERR_INVALID and "asl_" not in str(e.value)         # (by the checks, not by the library)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.int16, torch.uint16, torch.float32, torch.uint8])
+def test_rows_that_are_not_bf16(dtype):
+    """Elements of two bytes are not all bf16: float16 rows would be read as other numbers."""
+    c, b = bare(), a_batch()
+    q, rows, out = torch.zeros((2, 4, 128), dtype=torch.bfloat16), torch.zeros((2, 2, 128), dtype=torch.bfloat16), torch.zeros((2, 4, 128), dtype=torch.bfloat16)
+    refused(lambda: c.attend(0, b, q.to(dtype)))
+    refused(lambda: c.attend(0, b, q, out.to(dtype)))
+    refused(lambda: c.append(0, b, rows.to(dtype), rows))
+    refused(lambda: c.append(0, b, rows, rows.to(dtype)))
+    refused(lambda: bare(codes=True).append(0, b, rows.to(torch.uint8), rows.to(dtype)))
+
+
+@pytest.mark.parametrize("dtype", [torch.int32, torch.float64, torch.bfloat16])
+def test_a_log_sum_that_is_not_fp32(dtype):
+    c, b, q = bare(), a_batch(), torch.zeros((2, 4, 128), dtype=torch.bfloat16)
+    refused(lambda: c.attend(0, b, q, q.clone(), torch.zeros((2, 4), dtype=dtype)))
