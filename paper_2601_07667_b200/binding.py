@@ -554,7 +554,7 @@ class PagedCache:
     """Pages of K and V for several layers, the slots' table, lengths and counts, all torch tensors, and the calls on them
     (``asl_pages_*``, ``asl_attend*``) on the current stream.  Made from sizes, or over tensors that the caller already
     has (``k``, ``v`` [n_layers][n_pages][H_k][page_size][d], ``table`` [max_seqs][max_pages], ``length`` [max_seqs],
-    ``refs`` [n_pages]; ``k`` of one-byte elements are E4M3 codes with ``k_scale`` [n_layers][H_k]).
+    ``refs`` [n_pages]; ``k`` of float8_e4m3fn, uint8 or int8 are E4M3 codes with ``k_scale`` [n_layers][H_k]).
 
     ``reserve(want)``, ``fork(parent)`` and ``trim(to)`` take one int32 per slot on the device (negative: leave the slot
     alone).  What does not fit is left out on the device and noted; ``check()`` waits and raises it."""
@@ -578,10 +578,10 @@ class PagedCache:
         self._look_at(k, table)
         if k.dim() != 5 or v.shape != k.shape or k.shape[3] != page_size or v.dtype != torch.bfloat16 or table.dim() != 2:
             raise AslError(ASL_ERR_INVALID, "PagedCache: k and v are [n_layers][n_pages][H_k][page_size][d]")
-        if k.element_size() == 1:
+        if k.dtype in self._codes:
             k_dtype = ASL_K_FP8_E4M3
         elif k.dtype != torch.bfloat16:
-            raise AslError(ASL_ERR_INVALID, "PagedCache: k is bf16 or one-byte codes")
+            raise AslError(ASL_ERR_INVALID, "PagedCache: k is bf16 or E4M3 codes (float8_e4m3fn, or their bits as uint8 or int8)")
         else:
             k_dtype = ASL_K_BF16
         if not (k.is_contiguous() and v.is_contiguous() and v.device == k.device):
@@ -609,6 +609,7 @@ class PagedCache:
         """What the calls' checks compare their arguments with."""
         torch = self.torch
         self._i32, self._bf16, self._f32 = torch.int32, torch.bfloat16, torch.float32
+        self._codes = (torch.uint8, torch.float8_e4m3fn, torch.int8)
         self._device, self._strides, self._slots, self._d, self._k_type = k.get_device(), {}, table.shape[0], k.shape[-1], k.dtype
 
     def _ints(self, x, what: str):
@@ -625,7 +626,7 @@ class PagedCache:
         """A [tokens][heads][d] tensor's strides."""
         if x.dim() != 3 or x.shape[0] < n_tokens or x.shape[1] != heads or x.shape[2] != self._d or x.stride(2) != 1:
             raise AslError(ASL_ERR_INVALID, f"{what}: [tokens][heads][d] with dense rows")
-        if (x.element_size() != 1 if codes else x.dtype is not self._bf16) or x.get_device() != self._device:
+        if (x.dtype not in self._codes if codes else x.dtype is not self._bf16) or x.get_device() != self._device:
             raise AslError(ASL_ERR_INVALID, f"{what}: element type or device")
         key = (x.stride(0), x.stride(1))
         got = self._strides.get(key)

@@ -43,3 +43,22 @@ def test_rows_that_are_not_bf16(dtype):
 def test_a_log_sum_that_is_not_fp32(dtype):
     c, b, q = bare(), a_batch(), torch.zeros((2, 4, 128), dtype=torch.bfloat16)
     refused(lambda: c.attend(0, b, q, q.clone(), torch.zeros((2, 4), dtype=dtype)))
+
+
+OTHER_BYTES = [torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.float8_e8m0fnu, torch.bool]
+
+
+@pytest.mark.parametrize("dtype", OTHER_BYTES)
+def test_bytes_that_are_no_e4m3_codes(dtype):
+    """Codes come as E4M3 or as their bits; other one-byte types would be read as other numbers."""
+    v = torch.zeros((2, 2, 128), dtype=torch.bfloat16)
+    refused(lambda: bare(codes=True).append(0, a_batch(), torch.zeros((2, 2, 128), dtype=torch.uint8).view(dtype), v))
+    k = torch.zeros((1, 4, 2, 16, 128), dtype=torch.uint8).view(dtype)
+    refused(lambda: B.PagedCache(page_size=16, k=k, v=torch.zeros(k.shape, dtype=torch.bfloat16), table=torch.zeros((3, 4), dtype=torch.int32),
+                                 length=torch.zeros(3, dtype=torch.int32), refs=torch.zeros(4, dtype=torch.int32), k_scale=torch.ones((1, 2))))
+
+
+@pytest.mark.parametrize("dtype", [torch.uint8, torch.int8, torch.float8_e4m3fn])
+def test_codes_of_any_view(dtype):
+    k = torch.zeros((2, 2, 128), dtype=torch.uint8).view(dtype)
+    assert list(bare(codes=True)._rows(k, "k_new", 2, 2, True)) == [256, 128]
