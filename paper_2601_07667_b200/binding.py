@@ -419,7 +419,12 @@ class LayerPath:
         """From now on ``run_layer`` stores the kept rows into ``cache`` (layer ``layer_idx`` of it) instead of ``k_out`` and
         ``v_out``: request b's into slot ``slots[b]`` (device int32 [batch]), which ``cache.reserve`` has grown to ``kept[b]``
         tokens on the stream of the layers.  ``None``: into ``k_out`` and ``v_out`` again."""
-        self._pages = None if cache is None else (cache, slots)
+        if cache is None:
+            self._pages = None
+            return
+        if cache.dev != self.dev or slots is None or slots.numel() != self.batch:
+            raise AslError(ASL_ERR_INVALID, "store_into: a cache on the path's device, one slot per request")
+        self._pages = (cache, cache._ints(slots, "slots"))
 
     def set_controller(self, mode: int) -> None:
         """ASL_CONTROLLER_LATCH: selections are final on the device and ``run_layer`` tells the library the

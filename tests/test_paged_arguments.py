@@ -62,3 +62,27 @@ def test_bytes_that_are_no_e4m3_codes(dtype):
 def test_codes_of_any_view(dtype):
     k = torch.zeros((2, 2, 128), dtype=torch.uint8).view(dtype)
     assert list(bare(codes=True)._rows(k, "k_new", 2, 2, True)) == [256, 128]
+
+
+def a_path():
+    p = object.__new__(B.LayerPath)
+    p.torch, p.dev, p.batch, p.ctx, p._pages, p.H_k, p.sum_kept = torch, torch.device("cpu"), 2, 0, None, 2, 5
+    return p
+
+
+@pytest.mark.parametrize("slots", [None, torch.tensor([1, 0]), torch.tensor([1.0, 0.0]), torch.tensor([1], dtype=torch.int32), torch.tensor([1, 0, 2], dtype=torch.int32),
+                                   torch.tensor([1, 5, 0, 5], dtype=torch.int32)[::2]])
+def test_slots_to_store_into(slots):
+    """One dense int32 a request on the cache's device: int64 would be read as other slots, a host address not at all."""
+    c, p = bare(), a_path()
+    refused(lambda: p.store_into(c, slots))
+    assert p._pages is None
+    good = torch.tensor([1, 0], dtype=torch.int32)
+    p.store_into(c, good)
+    assert p._pages[0] is c and p._pages[1] is good
+    p.store_into(None)
+    assert p._pages is None
+    c._device = 0                                       # a cache on a device: host memory is not there
+    refused(lambda: p.store_into(c, good))
+    c, p.dev = bare(), torch.device("cuda", 1)
+    refused(lambda: p.store_into(c, good))
