@@ -627,12 +627,15 @@ class PagedCache:
             raise AslError(ASL_ERR_INVALID, f"{what}: one value per slot")
         return self._ints(x, what).data_ptr()
 
+    def _typed(self, x, what: str, codes: bool = False) -> None:
+        if (x.dtype not in self._codes if codes else x.dtype is not self._bf16) or x.get_device() != self._device:
+            raise AslError(ASL_ERR_INVALID, f"{what}: element type or device")
+
     def _rows(self, x, what: str, n_tokens: int, heads: int, codes: bool = False):
         """A [tokens][heads][d] tensor's strides."""
         if x.dim() != 3 or x.shape[0] < n_tokens or x.shape[1] != heads or x.shape[2] != self._d or x.stride(2) != 1:
             raise AslError(ASL_ERR_INVALID, f"{what}: [tokens][heads][d] with dense rows")
-        if (x.dtype not in self._codes if codes else x.dtype is not self._bf16) or x.get_device() != self._device:
-            raise AslError(ASL_ERR_INVALID, f"{what}: element type or device")
+        self._typed(x, what, codes)
         key = (x.stride(0), x.stride(1))
         got = self._strides.get(key)
         if got is None:
@@ -660,6 +663,7 @@ class PagedCache:
         """The kept rows of ``path``'s requests (``idx`` [H_k][sum_kept] as its top-k wrote them) into layer ``layer`` of the slots."""
         if idx.numel() != path.H_k * path.sum_kept or slots.numel() != path.batch:
             raise AslError(ASL_ERR_INVALID, "store: idx is [H_k][sum_kept], slots one per request")
+        self._typed(k, "k", self._k_type is not self._bf16), self._typed(v, "v")
         _check(_lib.asl_pages_store(path.ctx, self._ref, layer, k.data_ptr(), v.data_ptr(), self._ints(idx, "idx").data_ptr(),
                                     self._ints(slots, "slots").data_ptr(), _current_stream()), "asl_pages_store")
 

@@ -86,3 +86,17 @@ def test_slots_to_store_into(slots):
     refused(lambda: p.store_into(c, good))
     c, p.dev = bare(), torch.device("cuda", 1)
     refused(lambda: p.store_into(c, good))
+
+
+def test_a_prefills_rows_to_store():
+    """K and V of the cache's types, on its device (how they lie there the path's strides say)."""
+    c, p = bare(), a_path()
+    kv, idx, slots = torch.zeros((7, 2, 128), dtype=torch.bfloat16), torch.zeros((2, 5), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    for k, v in ((kv.half(), kv), (kv, kv.half()), (kv.view(torch.uint8), kv), (kv, kv.float())):
+        refused(lambda: c.store(0, p, k, v, idx, slots))
+    c = bare(codes=True)
+    codes = torch.zeros((7, 2, 128), dtype=torch.uint8)
+    for k, v in ((kv, kv), (codes.view(torch.float8_e5m2), kv), (codes, codes)):
+        refused(lambda: c.store(0, p, k, v, idx, slots))
+    c._device = 0
+    refused(lambda: c.store(0, p, codes, kv, idx, slots))
