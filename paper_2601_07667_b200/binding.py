@@ -545,7 +545,7 @@ class Batch:
         self.slots, self.cu_q = cache._ints(slots, "slots"), cache._ints(cu_q, "cu_q")
         if len(self.cu_q) != len(self.slots) + 1:
             raise AslError(ASL_ERR_INVALID, "batch: cu_q has one entry more than slots")
-        self.n_tokens, self.n_q_heads = int(n_tokens), n_q_heads
+        self.n_tokens, self.n_q_heads, self.device = int(n_tokens), n_q_heads, cache._device
         self.desc = AslBatch(len(self.slots), self.n_tokens, _ptr(self.slots), _ptr(self.cu_q))
         self.ref = C.byref(self.desc)
         self.workspace, self.ws, self.ws_bytes, self.share = None, 0, 0, 1
@@ -642,6 +642,11 @@ class PagedCache:
             got = self._strides[key] = (C.c_int64 * 2)(*key)
         return got
 
+    def _here(self, batch: Batch):
+        if batch.device != self._device:
+            raise AslError(ASL_ERR_INVALID, "batch: of a cache on another device")
+        return batch.ref
+
     def batch(self, slots, cu_q, n_tokens: int, n_q_heads: Optional[int] = None) -> Batch:
         """Sequences of a step: entry i is slot ``slots[i]`` (-1: padding) and owns tokens ``cu_q[i]`` .. ``cu_q[i+1]``, its last ones
         (device int32, read at every call).  ``n_q_heads``: also make the workspace that ``plan`` and ``attend`` need."""
@@ -680,14 +685,14 @@ class PagedCache:
         """K and V rows [n_tokens][H_k][d] of the batch's tokens, to the ends of their sequences."""
         ks = self._rows(k_new, "k_new", batch.n_tokens, self.pages.n_kv_heads, self._k_type is not self._bf16)
         vs = self._rows(v_new, "v_new", batch.n_tokens, self.pages.n_kv_heads)
-        _check(_lib.asl_pages_append(self.ctx, self._ref, layer, batch.ref, k_new.data_ptr(), v_new.data_ptr(), ks, vs,
+        _check(_lib.asl_pages_append(self.ctx, self._ref, layer, self._here(batch), k_new.data_ptr(), v_new.data_ptr(), ks, vs,
                                      _current_stream()), "asl_pages_append")
 
     def plan(self, batch: Batch, share: int = 1) -> None:
         """Deals out the attention of the step; again whenever lengths, pages or the batch have changed.  Prefixes that neighbours
         share are read once for all of them with ``share`` 1 where that saves enough, 2 wherever there are any, 0 nowhere."""
         batch.share = int(share)
-        _check(_lib.asl_attend_plan(self.ctx, self._ref, batch.ref, batch.n_q_heads or 0, batch.share, batch.ws, batch.ws_bytes,
+        _check(_lib.asl_attend_plan(self.ctx, self._ref, self._here(batch), batch.n_q_heads or 0, batch.share, batch.ws, batch.ws_bytes,
                                     _current_stream()), "asl_attend_plan")
 
     def attend(self, layer: int, batch: Batch, q, out=None, lse=None):
@@ -701,7 +706,7 @@ class PagedCache:
             raise AslError(ASL_ERR_INVALID, "out: dense [n_tokens][H_q][d] bf16")
         if lse is not None and (not lse.is_contiguous() or lse.numel() < n * heads or lse.dtype is not self._f32 or lse.get_device() != self._device):
             raise AslError(ASL_ERR_INVALID, "lse: dense [n_tokens][H_q] fp32")
-        _check(_lib.asl_attend(self.ctx, self._ref, layer, batch.ref, heads, batch.share, q.data_ptr(), strides, out.data_ptr(),
+        _check(_lib.asl_attend(self.ctx, self._ref, layer, self._here(batch), heads, batch.share, q.data_ptr(), strides, out.data_ptr(),
                                0 if lse is None else lse.data_ptr(), batch.ws, batch.ws_bytes, _current_stream()), "asl_attend")
         return out
 

@@ -8,7 +8,7 @@ from paper_2601_07667_b200 import binding as B
 
 def bare(codes=False):
     c = object.__new__(B.PagedCache)
-    c.torch, c.dev, c.ctx = torch, torch.device("cpu"), 0
+    c.torch, c.dev, c.ctx, c._ref = torch, torch.device("cpu"), 0, None
     k = torch.zeros((1, 4, 2, 16, 128), dtype=torch.uint8 if codes else torch.bfloat16)
     c._look_at(k, torch.zeros((3, 4), dtype=torch.int32))
     c.pages = B.AslPages(1, 2, 128, 16, 4, 3, 4, int(codes), None, None, None, None, None, None, None, None, 0)
@@ -17,7 +17,7 @@ def bare(codes=False):
 
 def a_batch(n_tokens=2, n_q_heads=4):
     b = object.__new__(B.Batch)
-    b.n_tokens, b.n_q_heads, b.share, b.ws, b.ws_bytes, b.ref = n_tokens, n_q_heads, 1, 0, 0, None
+    b.n_tokens, b.n_q_heads, b.share, b.ws, b.ws_bytes, b.ref, b.device = n_tokens, n_q_heads, 1, 0, 0, None, -1
     return b
 
 
@@ -100,3 +100,12 @@ def test_a_prefills_rows_to_store():
         refused(lambda: c.store(0, p, k, v, idx, slots))
     c._device = 0
     refused(lambda: c.store(0, p, codes, kv, idx, slots))
+
+
+def test_a_batch_of_another_device():
+    """Its slots and workspace lie where the cache's kernels do not look."""
+    c, b = bare(), a_batch()
+    q, rows = torch.zeros((2, 4, 128), dtype=torch.bfloat16), torch.zeros((2, 2, 128), dtype=torch.bfloat16)
+    b.device = 1
+    for call in (lambda: c.append(0, b, rows, rows), lambda: c.plan(b), lambda: c.attend(0, b, q)):
+        refused(call)
