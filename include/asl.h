@@ -447,8 +447,9 @@ asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, 
  * the stream, so that no other thread may launch on it meanwhile.  The workspace (asl_attend_workspace bytes, 256-byte
  * aligned) carries the plan and the parts of rows whose keys are split over several blocks; calls that share it have to be
  * ordered one behind another.
- * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its sizes writes nothing
- * and notes ASL_ERR_WORKSPACE; after an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
+ * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its cache and its sizes writes
+ * nothing and notes ASL_ERR_WORKSPACE (the first bytes of the plan say what it is for: zero 256 of a workspace that may hold old
+ * ones); after an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
 asl_status asl_attend_workspace(const asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, size_t* bytes);
 asl_status asl_attend_plan(asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, int32_t share,
                            void* workspace, size_t workspace_bytes, void* stream);

@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
     a.w.wide_start[k] = s;
   }
   if (tid == 0)
-    *a.w.head = {ATTEND_MARK, n, a.b.n_tokens, a.n_q_heads, H, 0, tiles, chunks, narrow_each, cost, wchunks, wide_each};
+    *a.w.head = {ATTEND_MARK, n, a.b.n_tokens, a.n_q_heads, H, a.g.page_shift, tiles, chunks, narrow_each, cost, wchunks, wide_each,
+                 a.g.max_seqs, a.g.max_pages, a.g.table};
 }
 
 // Rows whose keys were split: out = sum_i O_i 2^(m_i - m) / sum_i l_i 2^(m_i - m), m the largest m_i, and the same for lse.

@@ -18,9 +18,12 @@ constexpr int ATTEND_MAX_SEQS = 4096;
 
 struct __align__(16) AttendHead {        // one per plan, on the device
   int32_t mark, n_seqs, n_tokens, n_q_heads;          // what the layout follows from: see plan_fits
-  int32_t n_kv_heads, pad0, narrow_tiles, narrow_chunks;       // tiles and chunks per kv head
+  int32_t n_kv_heads, page_shift, narrow_tiles, narrow_chunks;       // tiles and chunks per kv head
   int32_t narrow_each, wide_cost, wide_chunks, wide_each;      // tiles and cost per CTA; cost and chunks per kv head
+  int32_t max_seqs, max_pages;             // of the cache whose slots the plan names, and its table
+  const int32_t* table;
 };
+static_assert(sizeof(AttendHead) == 64, "load_head reads four vectors");
 constexpr int ATTEND_MARK = 0x41534c50;
 struct __align__(16) AttendSeq {
   int32_t tok0, ntok, slot, len;       // ntok 0: padding
@@ -81,17 +84,18 @@ ASL_HD inline int wide_tokens(int G) { return WIDE_ROWS / G; }
 __device__ __forceinline__ AttendHead load_head(const AttendHead* h) {
   AttendHead r;
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < 4; ++i) {
     int4& q = reinterpret_cast<int4*>(&r)[i];
     asm volatile("ld.global.ca.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "l"(reinterpret_cast<const int4*>(h) + i) : "memory");
   }
   return r;
 }
-// A workspace that holds no plan, or one for other sizes, is refused before anything is read through it, and so is one with
-// shared prefixes where their kernel is not launched.
+// A workspace that holds no plan, or one for other sizes or another cache (whose slots this one's table may not have), is refused
+// before anything is read through it, and so is one with shared prefixes where their kernel is not launched.
 __device__ __forceinline__ bool plan_fits(const AttendArgs& a, const AttendHead& h) {
   const bool fits = h.mark == ATTEND_MARK && h.n_seqs == a.n_seqs && h.n_tokens == a.n_tokens && h.n_q_heads == a.n_q_heads &&
-                    h.n_kv_heads == a.g.n_kv_heads && (h.wide_cost == 0 || a.with_wide);
+                    h.n_kv_heads == a.g.n_kv_heads && h.page_shift == a.g.page_shift && h.max_seqs == a.g.max_seqs &&
+                    h.max_pages == a.g.max_pages && h.table == a.g.table && (h.wide_cost == 0 || a.with_wide);
   if (!fits && threadIdx.x == 0) note_error(a.g.err, ASL_ERR_WORKSPACE, -1);
   return fits;
 }
