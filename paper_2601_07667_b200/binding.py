@@ -552,6 +552,7 @@ class Batch:
         if n_q_heads is not None:
             self.ws_bytes = asl_attend_workspace(cache.ctx, cache.pages, self.desc, n_q_heads)
             self.workspace = cache.torch.empty(self.ws_bytes, dtype=cache.torch.uint8, device=cache.dev)
+            self.workspace[:256].zero_()               # no plan that an earlier owner of the memory left there
             self.ws = self.workspace.data_ptr()
 
 

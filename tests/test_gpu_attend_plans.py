@@ -1,4 +1,4 @@
-"""Plans that do not belong to the call that meets them."""
+"""Plans that do not belong to the call that meets them: of another cache, of an earlier owner of the workspace's memory."""
 import pytest
 import torch
 
@@ -54,3 +54,16 @@ def test_a_batch_may_serve_several_caches():
         both.cache.check()
         o, _, tol, _ = both.expect(0, list(range(34, 40)), list(range(7)), q.double().cpu().numpy(), 8)
         assert (abs(out.double().cpu().numpy() - o) <= tol).all()
+
+
+def test_a_plan_that_an_earlier_batch_left_is_none():
+    """A batch whose workspace lies where another's did, plan and all."""
+    both = forked(page=16, n_pages=80, max_seqs=40, max_pages=12)
+    slots, cu = ints(range(34, 40)), ints(range(7))
+    batch = both.cache.batch(slots, cu, n_tokens=6, n_q_heads=8)
+    both.cache.plan(batch)
+    at = batch.ws
+    del batch
+    batch = both.cache.batch(slots, cu, n_tokens=6, n_q_heads=8)
+    assert batch.ws == at
+    left_alone(both.cache, batch, 8)
