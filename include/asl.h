@@ -460,7 +460,9 @@ asl_status asl_attend(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const
                       size_t workspace_bytes, void* stream);
 
 /* asl_run_layer with its last step into pages: asl_pages_store on `side2` in asl_compact_kv's place (k_out and v_out of
- * `layer` are not looked at).  `slots` as in asl_pages_store, reserved before on a stream that `stream` is ordered behind. */
+ * `layer` are not looked at).  `slots` as in asl_pages_store, reserved before on a stream that `stream` is ordered behind.  The
+ * rows are in the cache for a stream that has been given to asl_run_join since: no other call on the cache before that (a fork
+ * that comes before the store makes the store leave out the rows, whose pages two slots then hold). */
 asl_status asl_run_layer_pages(asl_ctx* ctx, const asl_layer* layer, const asl_pages* pages, int32_t page_layer,
                                const int32_t* slots, const void* q_obs, const void* k, const void* v, const float* lse,
                                int32_t layer_idx, int32_t n_rows, int32_t slot);

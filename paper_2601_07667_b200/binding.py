@@ -418,7 +418,8 @@ class LayerPath:
     def store_into(self, cache: Optional["PagedCache"], slots=None) -> None:
         """From now on ``run_layer`` stores the kept rows into ``cache`` (layer ``layer_idx`` of it) instead of ``k_out`` and
         ``v_out``: request b's into slot ``slots[b]`` (device int32 [batch]), which ``cache.reserve`` has grown to ``kept[b]``
-        tokens on the stream of the layers.  ``None``: into ``k_out`` and ``v_out`` again."""
+        tokens on the stream of the layers.  The rows are stored on ``side2``: ``join`` before anything else is done with the cache
+        (a fork that comes before a store makes the store leave its rows out).  ``None``: into ``k_out`` and ``v_out`` again."""
         if cache is None:
             self._pages = None
             return
