@@ -340,10 +340,12 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
 template <bool CACHED>
 void launch_rows(const asl_ctx* c, const PagePool& g, const RowSource& x, const int32_t* idx, const int32_t* dst, int64_t sum_kept,
                  int max_kept, int jobs, cudaStream_t st) {
-  if ((int64_t)sum_kept * g.n_kv_heads >= (int64_t)c->sm_count * 4 * 256)
-    launch_after(rows_to_pages_kernel<CACHED, 256>, dim3((max_kept + 255) / 256, g.n_kv_heads, jobs), dim3(256), st, g, x, idx, dst, sum_kept);
+  const int64_t most = sum_kept < 1 ? 1 : max_kept < sum_kept ? max_kept : sum_kept;        // of one list
+  auto columns = [&](int rows) { return dim3((unsigned)((most + rows - 1) / rows), g.n_kv_heads, jobs); };
+  if (sum_kept * g.n_kv_heads >= (int64_t)c->sm_count * 4 * 256)
+    launch_after(rows_to_pages_kernel<CACHED, 256>, columns(256), dim3(256), st, g, x, idx, dst, sum_kept);
   else
-    launch_after(rows_to_pages_kernel<CACHED, 64>, dim3((max_kept + 63) / 64, g.n_kv_heads, jobs), dim3(256), st, g, x, idx, dst, sum_kept);
+    launch_after(rows_to_pages_kernel<CACHED, 64>, columns(64), dim3(256), st, g, x, idx, dst, sum_kept);
 }
 
 // A step's rows at the ends of their sequences: a block column per sequence, 16 threads a (token, kv head) row.

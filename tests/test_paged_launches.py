@@ -108,3 +108,12 @@ def test_no_plan_from_pages_that_were_not_compared(lib):
     assert c.kernels() == []
     assert c.plan(batch) == B.ASL_OK
     assert c.kernels() == ["attend_same_kernel", "attend_plan_kernel"]
+
+
+@pytest.mark.parametrize("sum_kept,max_kept,blocks", [(0, 100, 1), (1000, 1000, 16), (1000, 1, 1), (1000, 64, 1), (1000, 65, 2), (1000, 2 ** 31 - 1, 16), (2 ** 31 - 1, 2 ** 31 - 1, 1 << 23),
+                                                      (1 << 40, 2 ** 31 - 1, 1 << 23)])
+def test_lists_to_prune_by_of_any_announced_length(lib, sum_kept, max_kept, blocks):
+    """No list is longer than all of them together, and the columns of blocks are counted without running over."""
+    c = Cache(lib)
+    assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, A, 3, A, sum_kept, max_kept, None) == B.ASL_OK
+    assert c.launches() == [("rows_to_pages_kernel", blocks, 2, 3, 256, 0)]
