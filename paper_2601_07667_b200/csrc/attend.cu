@@ -532,7 +532,8 @@ asl_status asl_attend(asl_ctx* c, const asl_pages* p, int32_t layer, const asl_b
   asl_status s = check_attend(c, p, b, n_q_heads);
   if (s != ASL_OK) return s;
   if (!asl_on_device(c) || share < 0 || share > 2) return ASL_ERR_INVALID;
-  if (layer < 0 || layer >= p->n_layers || !q || !out || !q_stride || !asl_aligned16(q) || !asl_aligned16(out)) return ASL_ERR_INVALID;
+  if (b->n_tokens != 0 && (!q || !out)) return ASL_ERR_INVALID;     // (what is empty has no address)
+  if (layer < 0 || layer >= p->n_layers || !q_stride || !asl_aligned16(q) || !asl_aligned16(out)) return ASL_ERR_INVALID;
   for (int i = 0; i < 2; ++i)
     if (q_stride[i] < p->head_dim || q_stride[i] % 8) return ASL_ERR_INVALID;
   const AttendLayout l = layout_of(c->sm_count, p->n_kv_heads, b->n_seqs, b->n_tokens, n_q_heads);

@@ -504,7 +504,8 @@ asl_status asl_pages_append(asl_ctx* c, const asl_pages* p, int32_t layer, const
                             const int64_t k_stride[2], const int64_t v_stride[2], void* stream) {
   const asl_status s = check_call(c, p, layer);
   if (s != ASL_OK) return s;
-  if (!b || !b->slots || !b->cu_q || !k_new || !v_new || !k_stride || !v_stride) return ASL_ERR_INVALID;
+  if (!b || !b->slots || !b->cu_q || !k_stride || !v_stride) return ASL_ERR_INVALID;
+  if (b->n_tokens != 0 && (!k_new || !v_new)) return ASL_ERR_INVALID;             // (what is empty has no address)
   if (b->n_seqs < 1 || b->n_tokens < 0 || !asl_aligned16(k_new) || !asl_aligned16(v_new)) return ASL_ERR_INVALID;
   if (b->n_seqs > 4096) return ASL_ERR_UNSUPPORTED;
   const int kb = p->k_dtype == ASL_K_FP8_E4M3 ? 1 : 2;

@@ -38,3 +38,20 @@ def test_a_batch_whose_plan_is_about_48_kb(n):
     both.fork([i - 1 if i % 3 == 0 and i else -1 for i in range(n)])
     check_attention(both, 0, list(range(n)), list(range(n + 1)), 2, share=2)
     both.cache.close()
+
+
+def test_a_step_without_tokens():
+    """Every sequence has ended: a batch of padding and of free slots without a token, through every call of a step."""
+    both = Both(kv_heads=2, page=16, n_pages=20, max_seqs=4, max_pages=8)
+    both.fill([20, 0, 40, 0])
+    c = both.cache
+    batch = c.batch(ints([-1, 0, 1]), ints([0, 0, 0, 0]), n_tokens=0, n_q_heads=4)
+    rows, q = torch.empty((0, 2, 128), dtype=torch.bfloat16, device="cuda"), torch.empty((0, 4, 128), dtype=torch.bfloat16, device="cuda")
+    c.append(0, batch, rows, rows)
+    for share in (0, 1, 2):
+        c.plan(batch, share=share)
+        out = c.attend(0, batch, q, lse=torch.empty((0, 4), device="cuda"))
+        assert out.shape == (0, 4, 128)
+    c.check()
+    both.same_books()
+    both.same_rows()

@@ -117,3 +117,18 @@ def test_lists_to_prune_by_of_any_announced_length(lib, sum_kept, max_kept, bloc
     c = Cache(lib)
     assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, A, 3, A, sum_kept, max_kept, None) == B.ASL_OK
     assert c.launches() == [("rows_to_pages_kernel", blocks, 2, 3, 256, 0)]
+
+
+def test_a_step_without_tokens(lib):
+    """Empty tensors have no address: nothing is read, nothing launched, and the other arguments are looked at as ever."""
+    c, two = Cache(lib), (C.c_int64 * 2)(512, 128)
+    batch, heads, size = c.batch(3, 0)
+    assert lib.asl_pages_append(c.ctx, c.ref, 0, batch, None, None, two, two, None) == B.ASL_OK
+    assert lib.asl_attend(c.ctx, c.ref, 0, batch, heads, 1, None, two, None, None, A, size, None) == B.ASL_OK
+    assert lib.asl_pages_append(c.ctx, c.ref, 2, batch, None, None, two, two, None) == B.ASL_ERR_INVALID
+    assert lib.asl_attend(c.ctx, c.ref, 2, batch, heads, 1, None, two, None, None, A, size, None) == B.ASL_ERR_INVALID
+    assert lib.asl_attend(c.ctx, c.ref, 0, batch, heads, 1, None, two, None, None, A, size - 1, None) == B.ASL_ERR_WORKSPACE
+    batch, heads, size = c.batch(3, 1)
+    assert lib.asl_pages_append(c.ctx, c.ref, 0, batch, None, A, two, two, None) == B.ASL_ERR_INVALID
+    assert lib.asl_attend(c.ctx, c.ref, 0, batch, heads, 1, None, two, A, None, A, size, None) == B.ASL_ERR_INVALID
+    assert c.kernels() == []
