@@ -418,7 +418,8 @@ asl_status asl_pages_store(asl_ctx* ctx, const asl_pages* pages, int32_t layer, 
  * kv head by kv head (src, dst: device [n_jobs]; off: device [n_jobs + 1]; idx: device int32 [H_k][sum_kept], token
  * positions as asl_select_topk writes them; max_kept: at least the longest list).  dst[j] is another slot than src[j],
  * reserved before; asl_pages_trim then gives src[j] back.  Left out and noted: rows as in asl_pages_store, positions
- * that src[j] does not have.  Each dst once. */
+ * that src[j] does not have, lists that are not within [0, sum_kept), what a list has beyond the blocks for max_kept rows.
+ * Each dst once. */
 asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const int32_t* src, const int32_t* dst,
                              const int32_t* off, int32_t n_jobs, const int32_t* idx, int64_t sum_kept, int32_t max_kept,
                              void* stream);

@@ -271,12 +271,13 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
   if (CACHED) {
     src = __ldcg(x.src + b);
     const int o = __ldcg(x.off + b);
-    kept = __ldcg(x.off + b + 1) - o;
+    const int end = __ldcg(x.off + b + 1);
     at = o;
-    if (o < 0 || (int64_t)o + kept > sum_kept) kept = 0;
+    const bool listed = o >= 0 && o <= end && end <= sum_kept;
+    kept = listed ? end - o : 0;
     const bool fits = (unsigned)src < (unsigned)g.max_seqs && src != slot;
     n_src = fits ? min(__ldcg(g.len + src), g.max_pages << g.page_shift) : 0;
-    if (blockIdx.x == 0 && h == 0 && tid == 0 && kept > gridDim.x * R) note_error(g.err, ASL_ERR_INVALID, slot);     // more than max_kept
+    if (blockIdx.x == 0 && h == 0 && tid == 0 && (!listed || kept > (int64_t)gridDim.x * R)) note_error(g.err, ASL_ERR_INVALID, slot);     // or more than max_kept
   } else {
     if (x.latch && asl_finished(x.latch + b, x.cur_layer)) return;
     const AslReq rq = x.req[b];
@@ -340,7 +341,7 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
 template <bool CACHED>
 void launch_rows(const asl_ctx* c, const PagePool& g, const RowSource& x, const int32_t* idx, const int32_t* dst, int64_t sum_kept,
                  int max_kept, int jobs, cudaStream_t st) {
-  const int64_t most = sum_kept < 1 ? 1 : max_kept < sum_kept ? max_kept : sum_kept;        // of one list
+  const int64_t most = max_kept < 1 || sum_kept < 1 ? 1 : max_kept < sum_kept ? max_kept : sum_kept;        // of one list
   auto columns = [&](int rows) { return dim3((unsigned)((most + rows - 1) / rows), g.n_kv_heads, jobs); };
   if (sum_kept * g.n_kv_heads >= (int64_t)c->sm_count * 4 * 256)
     launch_after(rows_to_pages_kernel<CACHED, 256>, columns(256), dim3(256), st, g, x, idx, dst, sum_kept);
@@ -491,8 +492,7 @@ asl_status asl_pages_compact(asl_ctx* c, const asl_pages* p, int32_t layer, cons
                              void* stream) {
   const asl_status s = check_call(c, p, layer);
   if (s != ASL_OK) return s;
-  if (!src || !dst || !off || !idx || n_jobs < 1 || n_jobs > 65535 || sum_kept < 0 || max_kept < 0) return ASL_ERR_INVALID;
-  if (max_kept == 0) return ASL_OK;
+  if (!src || !dst || !off || (sum_kept != 0 && !idx) || n_jobs < 1 || n_jobs > 65535 || sum_kept < 0 || max_kept < 0) return ASL_ERR_INVALID;
   RowSource x = {};
   x.src = src;
   x.off = off;

@@ -55,3 +55,34 @@ def test_a_step_without_tokens():
     c.check()
     both.same_books()
     both.same_rows()
+
+
+@pytest.mark.parametrize("off,max_kept", [([-2, 3, 6], 6), ([0, 3, 7], 6), ([0, 4, 2], 6), ([3, 9, 6], 6), ([0, 0, 2 ** 31 - 1], 6), ([-2 ** 31, 3, 6], 6)])
+def test_lists_that_are_not_there_are_noted(off, max_kept):
+    """A job whose list begins or ends outside all lists is left out and noted; the other one, where its list is good, is done."""
+    both = Both(kv_heads=1, page=16, n_pages=30, max_seqs=6, max_pages=4, seed=1)
+    both.fill([40, 30, 0, 0, 0, 0])
+    both.reserve([-1, -1, 10, 10, -1, -1])
+    idx = [3, 5, 9, 11, 17, 29]
+    both.cache.compact(0, ints([0, 1]), ints([2, 3]), ints(off), ints(idx)[None], max_kept=max_kept)
+    st, slot = B.asl_pages_status(both.cache.ctx, both.cache.pages)
+    good = [0 <= off[j] <= off[j + 1] <= 6 for j in range(2)]
+    assert st == B.ASL_ERR_INVALID and slot in [s for s, ok in zip((2, 3), good) if not ok]
+    for j, (s, d) in enumerate(((0, 2), (1, 3))):
+        if good[j]:
+            k, v = both.oracle.rows(both.oracle.k, 0, s, 0).copy(), both.oracle.rows(both.oracle.v, 0, s, 0).copy()
+            for r, t in enumerate(idx[off[j]:off[j + 1]]):
+                both.oracle.put(0, d, r, 0, k[t], v[t])
+    both.same_rows()
+
+
+def test_nothing_kept_of_any_sequence():
+    both = Both(kv_heads=2, page=16, n_pages=30, max_seqs=4, max_pages=4, seed=1)
+    both.fill([40, 30, 0, 0])
+    none = torch.empty((2, 0), dtype=torch.int32, device="cuda")
+    both.cache.compact(0, ints([0, 1]), ints([2, 3]), ints([0, 0, 0]), none, max_kept=0)
+    both.cache.check()
+    both.cache.compact(0, ints([0, 1]), ints([2, 3]), ints([0, 0, 1]), none, max_kept=0)
+    assert B.asl_pages_status(both.cache.ctx, both.cache.pages) == (B.ASL_ERR_INVALID, 3)
+    both.same_rows()
+    both.same_books()

@@ -132,3 +132,15 @@ def test_a_step_without_tokens(lib):
     assert lib.asl_pages_append(c.ctx, c.ref, 0, batch, None, A, two, two, None) == B.ASL_ERR_INVALID
     assert lib.asl_attend(c.ctx, c.ref, 0, batch, heads, 1, None, two, A, None, A, size, None) == B.ASL_ERR_INVALID
     assert c.kernels() == []
+
+
+def test_no_rows_to_prune_by(lib):
+    """Nothing kept of any job: an empty list of positions has no address, and a list that is there all the same is noted by the kernel."""
+    c = Cache(lib)
+    assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, A, 3, None, 0, 0, None) == B.ASL_OK
+    assert c.kernels() == ["rows_to_pages_kernel"]
+    assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, A, 3, None, 1, 0, None) == B.ASL_ERR_INVALID
+    assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, A, 3, None, 0, -1, None) == B.ASL_ERR_INVALID
+    assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, None, 3, A, 0, 0, None) == B.ASL_ERR_INVALID
+    assert lib.asl_pages_compact(c.ctx, c.ref, 0, A, A, A, 0, A, 0, 0, None) == B.ASL_ERR_INVALID
+    assert c.kernels() == []
