@@ -410,7 +410,8 @@ asl_status asl_pages_trim(asl_ctx* ctx, const asl_pages* pages, const int32_t* t
 /* Algorithm 1 (K[I], V[I]) into pages instead of dense buffers: token r of slot slots[b] gets row idx[h][kept_off_b + r]
  * of request b, kv head by kv head (slots: device int32 [batch]; the plan, k, v and idx as in asl_compact_kv; the
  * plan's H_k and k_dtype have to be the cache's).  The slots' pages come from an asl_pages_reserve before it; rows
- * beyond a slot's length or into a page that another slot holds too are left out and noted. */
+ * beyond a slot's length or into a page that another slot holds too are left out and noted, and so are requests that
+ * have a slot in common. */
 asl_status asl_pages_store(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const void* k, const void* v,
                            const int32_t* idx, const int32_t* slots, void* stream);
 
@@ -418,8 +419,8 @@ asl_status asl_pages_store(asl_ctx* ctx, const asl_pages* pages, int32_t layer, 
  * kv head by kv head (src, dst: device [n_jobs]; off: device [n_jobs + 1]; idx: device int32 [H_k][sum_kept], token
  * positions as asl_select_topk writes them; max_kept: at least the longest list).  dst[j] is another slot than src[j],
  * reserved before; asl_pages_trim then gives src[j] back.  Left out and noted: rows as in asl_pages_store, positions
- * that src[j] does not have, lists that are not within [0, sum_kept), what a list has beyond the blocks for max_kept rows.
- * Each dst once. */
+ * that src[j] does not have, lists that are not within [0, sum_kept), what a list has beyond the blocks for max_kept rows,
+ * jobs whose dst is also another's dst or src (jobs without rows do not count). */
 asl_status asl_pages_compact(asl_ctx* ctx, const asl_pages* pages, int32_t layer, const int32_t* src, const int32_t* dst,
                              const int32_t* off, int32_t n_jobs, const int32_t* idx, int64_t sum_kept, int32_t max_kept,
                              void* stream);

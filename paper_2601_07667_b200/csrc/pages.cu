@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
   __shared__ int from_s[R], to_s[R];
   pdl_wait_predecessor();
   const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x;
-  const int slot = __ldcg(dst + b);
+  const int slot = __ldcg(dst + b), jobs = gridDim.z;
   int kept, src = 0, n_src;
   int64_t at, tok_off = 0;
   if (CACHED) {
@@ -313,7 +313,15 @@ __global__ void __launch_bounds__(256) rows_to_pages_kernel(PagePool g, RowSourc
     from_s[tid] = from;
     to_s[tid] = to;
   }
-  __syncthreads();
+  // Jobs run side by side, so that a slot which another job with rows reads or writes cannot be written.  (The last threads look
+  // first: where rows are few they have nothing else to do.)
+  bool clash = false;
+  for (int j = 255 - tid; j < jobs; j += 256)
+    if ((j != b && __ldcg(dst + j) == slot) || (CACHED && __ldcg(x.src + j) == slot)) clash |= !CACHED || __ldcg(x.off + j + 1) > __ldcg(x.off + j);
+  if (__syncthreads_or(clash)) {
+    if (tid == 0) note_error(g.err, ASL_ERR_INVALID, slot);
+    return;
+  }
   const int c = tid % 16, k_vec = g.k_row / 16;
   const uint8_t* ks = CACHED ? g.k : x.k + tok_off * x.ks_t + (int64_t)h * x.ks_h;
   const uint8_t* vs = CACHED ? g.v : x.v + tok_off * x.vs_t + (int64_t)h * x.vs_h;

@@ -1,9 +1,13 @@
-"""The paged cache at sizes around what a kernel's shared memory holds by default."""
+"""The paged cache at its limits: sizes around what a kernel's shared memory holds by default, steps and lists without rows, lists
+and slots that do not fit."""
+import numpy as np
 import pytest
 import torch
 
 from paper_2601_07667_b200 import binding as B
+from paper_2601_07667_b200 import inputs as I
 
+from asl_check import make_path, to_dev
 from pages_check import Both, check_attention, ints
 
 pytestmark = pytest.mark.gpu
@@ -86,3 +90,56 @@ def test_nothing_kept_of_any_sequence():
     assert B.asl_pages_status(both.cache.ctx, both.cache.pages) == (B.ASL_ERR_INVALID, 3)
     both.same_rows()
     both.same_books()
+
+
+@pytest.mark.parametrize("n_jobs", [4, 300])
+def test_slots_that_another_job_needs_are_left_alone(n_jobs):
+    """Jobs run side by side: one that would write a slot whose rows another reads, or that another writes too, is left out and
+    noted; those of other slots are done, and a slot may be read by several."""
+    both = Both(kv_heads=2, page=16, n_pages=700, max_seqs=n_jobs + 6, max_pages=4, seed=2)
+    both.fill([40, 30, 20, 50] + [0] * (n_jobs + 2))
+    both.reserve([-1] * 4 + [10] * (n_jobs + 2))
+    src, dst = [0, 1, 1, 3] + [0] * (n_jobs - 4), [1, 4, 5, 5] + list(range(6, n_jobs + 2))
+    if n_jobs > 4:
+        src[-1], dst[-1] = 9, n_jobs + 4               # reads what another job writes: that one is left out
+    done = [j for j in range(n_jobs) if j not in (0, 2, 3) and not (n_jobs > 4 and dst[j] == 9)]
+    idx = np.stack([np.concatenate([np.sort(both.rng.choice(10, 5, replace=False)) for _ in range(n_jobs)]) for _ in range(2)])
+    both.cache.compact(0, ints(src), ints(dst), ints(range(0, 5 * n_jobs + 1, 5)), torch.from_numpy(idx.astype(np.int32)).cuda(), max_kept=5)
+    st, slot = B.asl_pages_status(both.cache.ctx, both.cache.pages)
+    assert st == B.ASL_ERR_INVALID and slot in (1, 5, 9)
+    for j in done:
+        for h in range(2):
+            k, v = both.oracle.rows(both.oracle.k, 0, src[j], h).copy(), both.oracle.rows(both.oracle.v, 0, src[j], h).copy()
+            for r in range(5):
+                both.oracle.put(0, dst[j], r, h, k[idx[h, 5 * j + r]], v[idx[h, 5 * j + r]])
+    both.same_rows()
+
+
+def test_a_job_without_rows_takes_no_slot_from_another():
+    """Empty lists read and write nothing: their slots may be anybody's."""
+    both = Both(kv_heads=1, page=16, n_pages=20, max_seqs=4, max_pages=4, seed=2)
+    both.fill([40, 30, 0, 0])
+    both.reserve([-1, -1, 10, -1])
+    k, v = both.oracle.rows(both.oracle.k, 0, 0, 0).copy(), both.oracle.rows(both.oracle.v, 0, 0, 0).copy()
+    both.cache.compact(0, ints([0, 2, 1]), ints([2, 0, 2]), ints([0, 3, 3, 3]), ints([7, 8, 30])[None], max_kept=3)
+    both.cache.check()
+    for r, t in enumerate((7, 8, 30)):
+        both.oracle.put(0, 2, r, 0, k[t], v[t])
+    both.same_rows()
+
+
+def test_requests_that_share_a_slot_are_not_stored():
+    wl = I.workload("C3", n_q_heads=8, n_kv_heads=2, window=32, seqlens=(100, 200, 150), budgets=(64, 64, 64), layers=1, l_min=1, l_obs=2)
+    x = I.layer_inputs(wl, 0, seed=3)
+    path = make_path(wl)
+    both = Both(kv_heads=2, page=16, n_pages=30, max_seqs=3, max_pages=6)
+    both.reserve([64, 64, -1])
+    idx = np.stack([np.concatenate([np.sort(both.rng.choice(n, 64, replace=False)) for n in (100, 200, 150)]) for _ in range(2)])
+    both.cache.store(0, path, to_dev(x["k"]), to_dev(x["v"]), torch.from_numpy(idx.astype(np.int32)).cuda(), ints([1, 0, 1]))
+    assert B.asl_pages_status(both.cache.ctx, both.cache.pages) == (B.ASL_ERR_INVALID, 1)
+    for h in range(2):
+        for r in range(64):
+            t = 100 + idx[h, 64 + r]
+            both.oracle.put(0, 0, r, h, x["k"][t, h], x["v"][t, h])
+    both.same_rows()
+    path.close()
