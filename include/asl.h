@@ -395,7 +395,7 @@ asl_status asl_pages_scratch(const asl_pages* pages, size_t* bytes);
  * are the lowest-numbered free ones, dealt out in the order of slots and of positions.  Where the slot's last page is
  * not full and another slot holds it too, the slot gets a copy of the tokens that it has there, in all layers.  The
  * new tokens' rows are whatever the pages held: asl_pages_append or asl_pages_store write them.  All or nothing: with
- * too few free pages (ASL_ERR_PAGES, with the number missing) or a want beyond max_pages * page_size (ASL_ERR_INVALID,
+ * too few free pages (ASL_ERR_PAGES, with the number missing, 2^31 - 1 at most) or a want beyond max_pages * page_size (ASL_ERR_INVALID,
  * with the slot) no slot grows. */
 asl_status asl_pages_reserve(asl_ctx* ctx, const asl_pages* pages, const int32_t* want, void* stream);
 

@@ -4,6 +4,8 @@
 // dependent loads and the launch (reserving 6 us, forking, cutting 3).  The rows are bound by HBM's rate for scattered 256-byte rows,
 // like compaction (half of four 24K-token prompts, 268 MB: 46 us, 5.8 TB/s), where they are many; a layer's few thousand (23 MB) by
 // four dependent loads (6.6 us).
+#include <limits.h>
+
 #include "pages.cuh"
 
 namespace {
@@ -82,6 +84,7 @@ __global__ void __launch_bounds__(TABLE_THREADS) pages_reserve_kernel(PagePool g
   extern __shared__ uint32_t bits[];       // one bit per page: free
   __shared__ int part[33];
   __shared__ int bad;
+  __shared__ unsigned long long all_s;
   pdl_wait_predecessor();
   const int tid = threadIdx.x, words = (g.n_pages + 31) / 32, page = 1 << g.page_shift;
   int4* cow = reinterpret_cast<int4*>(scratch + SCRATCH_HEAD);
@@ -137,8 +140,17 @@ __global__ void __launch_bounds__(TABLE_THREADS) pages_reserve_kernel(PagePool g
   int free_all;
   int at = block_scan(mine, part, free_all);
   if (bad) return;
-  if (need_all > free_all) {
-    if (tid == 0) note_error(g.err, ASL_ERR_PAGES, need_all - free_all);
+  if (need_all > free_all) {               // how many are missing: counted again, where no sum is clamped
+    unsigned long long need = 0;
+    for (int s = tid; s < g.max_seqs; s += TABLE_THREADS) {
+      const int n = __ldcg(g.len + s), w = __ldcg(want + s);
+      if (w > n) need += pages_for(w, g.page_shift) - pages_for(n, g.page_shift) + (off[s] < 0);
+    }
+    if (tid == 0) all_s = 0;
+    __syncthreads();
+    if (need) atomicAdd(&all_s, need);
+    __syncthreads();
+    if (tid == 0) note_error(g.err, ASL_ERR_PAGES, (int)min(all_s - free_all, (unsigned long long)INT_MAX));
     return;
   }
   if (need_all == 0) {                     // growth inside the last pages

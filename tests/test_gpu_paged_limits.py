@@ -143,3 +143,18 @@ def test_requests_that_share_a_slot_are_not_stored():
             both.oracle.put(0, 0, r, h, x["k"][t, h], x["v"][t, h])
     both.same_rows()
     path.close()
+
+
+@pytest.mark.parametrize("slots,each", [(3, 1 << 20), (40, 1 << 20), (1100, 3000), (2100, 1 << 20)])
+def test_how_many_pages_are_missing(slots, each):
+    """Wants of far more pages than any pool has are counted to the last page (2^31 - 1 stands for all above)."""
+    k = torch.zeros((1, 50, 1, 16, 128), dtype=torch.bfloat16, device="cuda")
+    length, refs = torch.zeros(slots, dtype=torch.int32, device="cuda"), torch.zeros(50, dtype=torch.int32, device="cuda")
+    cache = B.PagedCache(page_size=16, k=k, v=k.clone(), table=torch.zeros((slots, each), dtype=torch.int32, device="cuda"), length=length, refs=refs)
+    cache.reserve(ints([20] + [-1] * (slots - 1)))
+    cache.fork(ints([-1, 0] + [-1] * (slots - 2)))
+    cache.reserve(ints([each * 16] * slots))
+    # the first two need a page for the copy of what they share besides, and hold two already
+    missing = min(slots * each - 4 + 2 - 48, 2 ** 31 - 1)
+    assert B.asl_pages_status(cache.ctx, cache.pages) == (B.ASL_ERR_PAGES, missing)
+    assert length[:3].tolist() == [20, 20, 0] and refs.sum().item() == 4
