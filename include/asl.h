@@ -451,7 +451,8 @@ asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, 
  * ordered one behind another.
  * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its cache and its sizes writes
  * nothing and notes ASL_ERR_WORKSPACE (the first bytes of the plan say what it is for: zero 256 of a workspace that may hold old
- * ones); after an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
+ * ones).  Where the table names a page that the pool does not have, page 0 is read in its place and ASL_ERR_INVALID noted with the
+ * slot, whose rows, and those of the neighbours that share the page, are void.  After an ASL_ERR_TIMEOUT (asl_device_status: the kernels' waits are bounded) its rows are void. */
 asl_status asl_attend_workspace(const asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, size_t* bytes);
 asl_status asl_attend_plan(asl_ctx* ctx, const asl_pages* pages, const asl_batch* batch, int32_t n_q_heads, int32_t share,
                            void* workspace, size_t workspace_bytes, void* stream);

@@ -137,6 +137,12 @@ __device__ __forceinline__ AttendGroup load_group(const AttendGroup* s) {
   reinterpret_cast<int4*>(&r)[1] = __ldcg(reinterpret_cast<const int4*>(s) + 1);
   return r;
 }
+// A page number out of a table: one that the pool does not have is noted, and page 0 read in its place.
+__device__ __forceinline__ int page_in_pool(const PagePool& g, int id, int slot) {
+  if ((unsigned)id < (unsigned)g.n_pages) return id;
+  note_error(g.err, ASL_ERR_INVALID, slot);
+  return 0;
+}
 __device__ __forceinline__ int narrow_tiles_of(const AttendSeq& s) { return max(1, (s.len - s.pfx + NARROW_KEYS - 1) / NARROW_KEYS); }
 __device__ __forceinline__ int narrow_chunks_of(int ntok, int G) { return (ntok * G + NARROW_ROWS - 1) / NARROW_ROWS; }
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {

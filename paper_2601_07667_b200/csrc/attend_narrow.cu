@@ -165,7 +165,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
         const int p0 = key0 >> a.g.page_shift;
         if (p0 + (NARROW_KEYS - 1 >> a.g.page_shift) >= first + 32) {        // page numbers of the next tiles, a lane each
           first = p0;
-          ids = first + lane < end ? __ldcg(row + first + lane) : -1;
+          ids = first + lane < end ? page_in_pool(a.g, __ldcg(row + first + lane), w.s.slot) : 0;
         }
         if (n >= STAGES && !mbar_wait(empty(st), (n / STAGES - 1) & 1, s_abort, 201, true)) { more = false; break; }
         const int count = min(per, max(0, ((end << a.g.page_shift) - key0 + piece - 1) / piece));       // pieces of pages that it has
@@ -175,7 +175,6 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
           const int key = key0 + x * piece, pg = key >> a.g.page_shift;
           const int id = __shfl_sync(0xffffffffu, ids, (pg - first) & 31);
           if (pg < end && elect_one()) {
-            // (a page number out of range copies zeros or other rows of the pool, never from outside it)
             const int r = ((id * n_kv + w.h) << a.g.page_shift) + (key & ((1 << a.g.page_shift) - 1));
             // both 64-channel halves of a piece by one copy, one behind the other
             const uint32_t kd = base + st * S::STAGE, vd = kd + S::K_BYTES + x * piece * 256;

@@ -291,12 +291,12 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
         const int32_t* row = a.g.table + (int64_t)w.g.slot * a.g.max_pages;
         const int last = w.g.pfx >> shift;   // pages of the prefix
         int first = w.tile * per;            // page numbers of 32 pages a lane each, and of the 32 after them
-        int ids = first + lane < last ? __ldcg(row + first + lane) : 0;
+        int ids = first + lane < last ? page_in_pool(a.g, __ldcg(row + first + lane), w.g.slot) : 0;
         int ids2 = first + 32 + lane < last ? __ldcg(row + first + 32 + lane) : 0;
         for (int t = w.tile; t < w.end; ++t, ++n) {
           if (t * per >= first + 32) {       // (a tile has 8 pages at most, and 32 is a multiple of what it has)
             first += 32;
-            ids = ids2;
+            ids = page_in_pool(a.g, ids2, w.g.slot);           // (looked at no earlier: it comes while the tiles before are copied)
             ids2 = first + 32 + lane < last ? __ldcg(row + first + 32 + lane) : 0;
           }
           const int ks = n % K_RING, vs = n % S::V_RING, np = w.keys(t) >> shift;

@@ -1,10 +1,11 @@
-"""Plans that do not belong to the call that meets them: of another cache, of an earlier owner of the workspace's memory."""
+"""Plans that do not belong to the call that meets them: of another cache, of an earlier owner of the workspace's memory; and
+tables that name pages which the pool does not have."""
 import pytest
 import torch
 
 from paper_2601_07667_b200 import binding as B
 
-from pages_check import Both, check_attention, ints
+from pages_check import Both, check_attention, ints, queries
 
 pytestmark = pytest.mark.gpu
 
@@ -67,3 +68,39 @@ def test_a_plan_that_an_earlier_batch_left_is_none():
     batch = both.cache.batch(slots, cu, n_tokens=6, n_q_heads=8)
     assert batch.ws == at
     left_alone(both.cache, batch, 8)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("page,prompt", [(16, 90), (16, 1500), (128, 300)])
+@pytest.mark.parametrize("wrong", [-1, "n_pages", 1 << 30, -2 ** 31])
+def test_page_numbers_that_the_pool_does_not_have(page, prompt, wrong, fp8):
+    """A spoiled entry of the table, in a tail or in the pages that a prompt's forks share (the first ones or far behind them): noted
+    with a slot that holds it; what does not read it is as it was."""
+    n_pages = 6 + -(-prompt // page) + 5 * 3 + 2
+    both = Both(kv_heads=2, page=page, n_pages=n_pages, max_seqs=8, max_pages=-(-prompt // page) + 2, fp8=fp8, seed=3)
+    both.fill([prompt, 0, 0, 0, 0, 0, 40, 0])
+    both.fork([-1, 0, 0, 0, 0, 0, -1, -1])
+    both.fill([-1] + [prompt + 1 + i for i in range(5)] + [-1, -1])
+    slots, cu = list(range(1, 7)), list(range(7))
+    q = queries(both.rng, 6, 8)
+    clean = {share: check_attention(both, 0, slots, cu, 8, share=share, q=q)[1] for share in (0, 2)}
+    batch = both.cache.batch(ints(slots), ints(cu), n_tokens=6, n_q_heads=8)
+    wrong = n_pages if wrong == "n_pages" else wrong
+    table, last = both.cache.table.clone(), prompt // page
+    for spoiled, column in (([3], last), ([1, 2, 3, 4, 5], 0), ([1, 2, 3, 4, 5], last - 1), ([6], 0)):
+        both.cache.table[torch.tensor(spoiled), column] = wrong
+        for share in (0, 2):
+            both.cache.plan(batch, share=share)
+            out = both.cache.attend(0, batch, q[0])
+            st, slot = B.asl_pages_status(both.cache.ctx, both.cache.pages)
+            assert st == B.ASL_ERR_INVALID and slot in spoiled
+            for i, s in enumerate(slots):
+                if s not in spoiled:
+                    assert torch.equal(out[i], clean[share][i]) or both_close(both, s, out[i], q[1][i])
+        both.cache.table.copy_(table)
+
+
+def both_close(both, slot, out, q):
+    """Neighbours that no longer share what they did are read in other parts, and still within the tolerance."""
+    o, _, tol, _ = both.expect(0, [slot], [0, 1], q[None], 8)
+    return (abs(out[None].double().cpu().numpy() - o) <= tol).all()
