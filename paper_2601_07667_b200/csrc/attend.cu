@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) attend_plan_kernel(PlanArgs a) {
   int32_t* gchunk = sm + 9 * n;
   int32_t* first = sm + 10 * n;            // [n + 1] narrow tiles before
   int32_t* gcost = sm + 11 * n + 1;        // [n + 1] wide cost before
-  if (tid == 0) { a.w.head->mark = 0; most_s = 0; any_full = 0; bad = 0; }
+  if (tid == 0) { a.w.head->mark = 0; *a.w.open = 0; most_s = 0; any_full = 0; bad = 0; }
   for (int t = tid; t < a.b.n_tokens; t += PLAN_THREADS) a.w.tokens[t].seq.ntok = 0;
   __syncthreads();
   unsigned long long most = 0;             // tiles, were nothing shared: they are counted in 32 bits
@@ -316,6 +316,7 @@ template <int WARPS>
 __global__ void __launch_bounds__(128) attend_join_kernel(AttendArgs a) {
   __shared__ float4 joined[4][32];
   pdl_wait_predecessor();
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.w.open = 0;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = WARPS == 1 ? 0 : warp;
   const int row = WARPS == 1 ? blockIdx.x * 4 + warp : blockIdx.x;
   const bool exists = row < a.n_tokens * a.n_q_heads;
@@ -435,7 +436,8 @@ AttendLayout layout_of(int sm_count, int n_kv_heads, int n_seqs, int n_tokens, i
   const size_t narrow_slots = (size_t)(H * narrow + l.narrow_grid), wide_slots = (size_t)(H * wide + 3 * l.wide_grid);
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t at = off; off = asl_align256(off + bytes); return at; };
-  l.head = take(sizeof(AttendHead));
+  l.head = take(128 + sizeof(uint32_t));
+  l.open = l.head + 128;                   // (a line of its own: the head is read through L1)
   l.seqs = take(sizeof(AttendSeq) * n_seqs);
   l.groups = take(sizeof(AttendGroup) * n_seqs);
   l.same = take(sizeof(int32_t) * n_seqs);
@@ -453,6 +455,7 @@ AttendPtrs ptrs_of(const AttendLayout& l, void* workspace) {
   char* w = static_cast<char*>(workspace);
   AttendPtrs p;
   p.head = reinterpret_cast<AttendHead*>(w + l.head);
+  p.open = reinterpret_cast<uint32_t*>(w + l.open);
   p.seqs = reinterpret_cast<AttendSeq*>(w + l.seqs);
   p.groups = reinterpret_cast<AttendGroup*>(w + l.groups);
   p.same = reinterpret_cast<int32_t*>(w + l.same);

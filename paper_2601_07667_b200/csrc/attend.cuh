@@ -43,13 +43,14 @@ struct __align__(16) AttendStart {
 };
 
 struct AttendLayout {      // byte offsets in the workspace
-  size_t head, seqs, groups, same, tokens, narrow_start, wide_start, ml, o, total;
+  size_t head, open, seqs, groups, same, tokens, narrow_start, wide_start, ml, o, total;
   int64_t wide_row0;
   int32_t narrow_grid, wide_grid;
 };
 
 struct AttendPtrs {
   AttendHead* head;
+  uint32_t* open;          // 1 while the prefixes' kernel of a call has seen the end of all before it, else 0 (see narrow_may_read)
   AttendSeq* seqs;
   AttendGroup* groups;
   int32_t* same;           // [n_seqs] leading pages that an entry has in common with the one before
@@ -79,6 +80,18 @@ struct AttendArgs {
 ASL_HD inline int wide_tokens(int G) { return WIDE_ROWS / G; }
 
 #ifdef __CUDACC__
+// The kernel of the sequences' own keys runs beside the prefixes' one, which has waited for all before it and writes nothing that
+// it reads.  griddepcontrol makes earlier grids' writes visible only behind a wait of its own, which would be for the end of the
+// prefixes' kernel too (five prefixes' cases: 115 -> 121, 159 -> 169, 355 -> 373, 137 -> 149, 67 -> 73 us).  So the one that has
+// waited says so by a release, behind which all that it may see is seen by who acquires it; who does not find it said waits.  The
+// kernel that joins the parts takes it back.
+__device__ __forceinline__ void others_may_read(uint32_t* open) { asm volatile("st.release.gpu.global.u32 [%0], 1;" ::"l"(open) : "memory"); }
+__device__ __forceinline__ bool narrow_may_read(const uint32_t* open) {        // by a whole warp
+  uint32_t v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(open) : "memory");
+  asm volatile("fence.proxy.async;" ::: "memory");                             // (its copies read by the async proxy)
+  return __all_sync(0xffffffffu, v == 1u);
+}
 // Every warp reads the head: by loads that L1 keeps (written two launches ago or more), since thousands of requests for one
 // line wait for one another in L2 (the joined rows of 32 sequences with 32 heads: 13 us, of which 8.7 were these loads).
 __device__ __forceinline__ AttendHead load_head(const AttendHead* h) {

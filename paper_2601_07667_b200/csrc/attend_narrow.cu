@@ -114,6 +114,9 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
   auto empty = [&](int st) { return base + S::BARS + 8 * (STAGES + st); };
   const uint32_t q_full = base + S::BARS + 8 * S::QF, q_empty = base + S::BARS + 8 * S::QE;
   Part* part = reinterpret_cast<Part*>(sm + S::PART);
+  // Behind the prefixes' kernel (`beside`) the copying warp, from which the others have all that they know, asks whether that kernel
+  // has seen the end of all before it; neither writes what the other reads.
+  const bool may_read = !beside || warp != WARPS || narrow_may_read(a.w.open);
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), WARPS); }
     mbar_init(q_full, 1);
@@ -122,9 +125,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncthreads();
-  // Behind the prefixes' kernel (`beside`) nothing is waited for: that kernel lets this one start only when all before it is
-  // done, and neither writes what the other reads.
-  if (!beside) pdl_wait_predecessor();
+  if (!beside || !may_read) pdl_wait_predecessor();
   const int n_kv = a.g.n_kv_heads, G = a.group_heads;
   if (warp == WARPS) {
     Walk w;

@@ -104,3 +104,38 @@ def both_close(both, slot, out, q):
     """Neighbours that no longer share what they did are read in other parts, and still within the tolerance."""
     o, _, tol, _ = both.expect(0, [slot], [0, 1], q[None], 8)
     return (abs(out[None].double().cpu().numpy() - o) <= tol).all()
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_steps_back_to_back_read_what_was_just_written(fp8):
+    """Rows appended, queries changed and attention over a shared prefix and tails, call behind call without a wait: the same bits as
+    with a wait behind each.  The word by which one kernel lets the next one read is taken back every time."""
+    n, L = 24, 2
+    both = Both(kv_heads=4, page=16, n_pages=400, max_seqs=n + 1, max_pages=80, layers=L, fp8=fp8, seed=9)
+    both.fill([1030] + [0] * n)
+    both.fork([-1] + [0] * n)
+    both.fill([-1] + [1031 + 7 * i % 60 for i in range(n)])
+    c = both.cache
+    batch = c.batch(ints(range(1, n + 1)), ints(range(n + 1)), n_tokens=n, n_q_heads=16)
+    steps = [([both.dev(x) for x in both.new_rows(n, 4, 128)], queries(both.rng, n, 16)[0]) for _ in range(12)]
+    word = batch.workspace[128:132].view(torch.int32)
+
+    def go(wait):
+        got = []
+        for (k, v), q in steps:
+            for layer in range(L):
+                c.append(layer, batch, k, v)
+                if wait:
+                    torch.cuda.synchronize()
+            c.plan(batch, share=2)
+            for layer in range(L):
+                got.append(c.attend(layer, batch, q))
+                if wait:
+                    torch.cuda.synchronize()
+                    assert word.item() == 0
+        return got
+    waited = go(True)
+    for _ in range(8):
+        for a, b in zip(waited, go(False)):
+            assert torch.equal(a, b)
+    c.check()
