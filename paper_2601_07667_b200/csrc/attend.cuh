@@ -69,7 +69,7 @@ struct AttendArgs {
   int64_t qs_t, qs_h;      // element strides
   __nv_bfloat16* out;
   float* lse;              // or null
-  const float* k_scale;    // [H_k] of the layer, or null
+  const float* k_scale;    // [H_k] of the layer, or null; the kernel before may write it, so that it is read by coherent loads
   int32_t* err;            // the context's word of bounded waits
   int32_t n_q_heads, group_heads, n_tokens, n_seqs;
   int32_t with_wide;       // the prefixes' kernel is launched
@@ -92,8 +92,8 @@ __device__ __forceinline__ bool narrow_may_read(const uint32_t* open) {        /
   asm volatile("fence.proxy.async;" ::: "memory");                             // (its copies read by the async proxy)
   return __all_sync(0xffffffffu, v == 1u);
 }
-// Every warp reads the head: by loads that L1 keeps (written two launches ago or more), since thousands of requests for one
-// line wait for one another in L2 (the joined rows of 32 sequences with 32 heads: 13 us, of which 8.7 were these loads).
+// Every warp reads the head, behind its kernel's wait (or acquire) for the one that wrote it: by loads that L1 keeps, since thousands
+// of requests for one line wait for one another in L2 (the joined rows of 32 sequences with 32 heads: 13 us, of which 8.7 were these loads).
 __device__ __forceinline__ AttendHead load_head(const AttendHead* h) {
   AttendHead r;
 #pragma unroll

@@ -211,7 +211,7 @@ attend_narrow_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_cons
       const Part w = *part;
       if (w.tiles == 0) break;
       const int nt = w.tiles;
-      const float c = a.scale_log2 * (FP8 ? __ldg(a.k_scale + w.h) : 1.0f);
+      const float c = a.scale_log2 * (FP8 ? __ldcg(a.k_scale + w.h) : 1.0f);
       const int rows = w.ntok * G, lr0 = w.chunk * NARROW_ROWS;
       // the chunk's rows gid and gid + 8: token, keys it sees (rows that do not exist: none)
       int lim[2], tok[2];

@@ -170,7 +170,7 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
       const bool full = w.full();
       const int r = full ? s * 128 + row : row;                     // row of the chunk
       const bool warp_has = (r & ~31) < w.rows;                     // of this warp's rows some exist
-      const float c = a.scale_log2 * (FP8 ? __ldg(a.k_scale + w.h) : 1.0f);
+      const float c = a.scale_log2 * (FP8 ? __ldcg(a.k_scale + w.h) : 1.0f);
       float m = -INFINITY;
       f32x2 l2 = pk(0.0f, 0.0f);
       const int t0 = full ? w.tile : w.tile + s, dt = full ? 1 : 2;

@@ -139,3 +139,25 @@ def test_steps_back_to_back_read_what_was_just_written(fp8):
         for a, b in zip(waited, go(False)):
             assert torch.equal(a, b)
     c.check()
+
+
+def test_scales_may_change_from_call_to_call():
+    """Key scales written by the kernel just before: the calls behind it use them."""
+    both = Both(kv_heads=2, page=16, n_pages=200, max_seqs=9, max_pages=44, fp8=True, seed=2)
+    both.fill([600] + [0] * 8)
+    both.fork([-1] + [0] * 8)
+    both.fill([-1] + [601 + 9 * i for i in range(8)])
+    slots, cu, q = list(range(1, 9)), list(range(9)), queries(both.rng, 8, 8)
+    batch = both.cache.batch(ints(slots), ints(cu), n_tokens=8, n_q_heads=8)
+    first = both.scale.copy()
+    for share in (0, 2):
+        both.cache.plan(batch, share=share)
+        outs = []
+        for times in (1.0, 2.0, 0.5, 1.5):
+            both.cache.k_scale.copy_(torch.from_numpy(first).cuda() * times)
+            outs.append((times, both.cache.attend(0, batch, q[0])))
+        for times, out in outs:
+            both.scale = first * times
+            o, _, tol, _ = both.expect(0, slots, cu, q[1], 8)
+            assert (abs(out.double().cpu().numpy() - o) <= tol).all()
+    both.cache.check()
