@@ -651,7 +651,8 @@ class PagedCache:
 
     def batch(self, slots, cu_q, n_tokens: int, n_q_heads: Optional[int] = None) -> Batch:
         """Sequences of a step: entry i is slot ``slots[i]`` (-1: padding) and owns tokens ``cu_q[i]`` .. ``cu_q[i+1]``, its last ones
-        (device int32, read at every call).  ``n_q_heads``: also make the workspace that ``plan`` and ``attend`` need."""
+        (device int32, read at every call).  ``n_q_heads``: also make the workspace that ``plan`` and ``attend`` need (its head is cleared
+        on the current stream)."""
         return Batch(self, slots, cu_q, n_tokens, n_q_heads)
 
     def reserve(self, want) -> None:
