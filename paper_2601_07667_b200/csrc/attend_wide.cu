@@ -153,8 +153,10 @@ attend_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_consta
   tc_fence_after();
   const uint32_t tmem = *reinterpret_cast<const uint32_t*>(sm + S::MISC);
   pdl_wait_predecessor();
-  if (blockIdx.x == 0 && threadIdx.x == 0) others_may_read(a.w.open);
-  pdl_release_successor();                 // it finds room when this grid's blocks leave
+  if (threadIdx.x == 0) {
+    if (blockIdx.x == 0) others_may_read(a.w.open);      // (before it starts)
+    pdl_release_successor();               // it finds room when this grid's blocks leave
+  }
   const int G = a.group_heads, T = wide_tokens(G);
 
   if (warp >= 4 && warp < 12) {
