@@ -79,6 +79,27 @@ struct AttendArgs {
 // Tokens of a chunk of a group's rows (at least two, since a token has at most 128).
 ASL_HD inline int wide_tokens(int G) { return WIDE_ROWS / G; }
 
+// A group's tiles, chunks and cost.  All chunks but the last have as many tokens as fit (and more than 128 rows).
+struct WideShape {
+  int tiles, whole, rest, chunks, stripe, stripes;
+  int sum;                                 // cost of one tile of every chunk
+  ASL_HD inline WideShape(int ntok, int pfx, int G, int stripe_) {
+    const int T = wide_tokens(G);
+    tiles = (pfx + WIDE_KEYS - 1) / WIDE_KEYS;
+    whole = ntok / T;
+    rest = ntok - whole * T;
+    chunks = whole + (rest > 0);
+    sum = 2 * whole + (rest ? weight_of(rest, G) : 0);
+    stripe = chunks > 1 && stripe_ < tiles ? stripe_ : tiles;        // (so that stripe x sum is no more than the group's cost)
+    stripes = tiles ? (tiles + stripe - 1) / stripe : 0;
+  }
+  static ASL_HD inline int weight_of(int tokens, int G) { return tokens * G > WIDE_ROWS / 2 ? 2 : 1; }
+  ASL_HD inline int weight(int chunk, int G) const { return chunk < whole ? 2 : weight_of(rest, G); }
+  ASL_HD inline int tiles_of(int s) const { return tiles - s * stripe < stripe ? tiles - s * stripe : stripe; }
+  // cost before a chunk of a stripe
+  ASL_HD inline int before(int s, int chunk) const { return s * stripe * sum + tiles_of(s) * 2 * chunk; }
+};
+
 #ifdef __CUDACC__
 // The kernel of the sequences' own keys runs beside the prefixes' one, which has waited for all before it and writes nothing that
 // it reads.  griddepcontrol makes earlier grids' writes visible only behind a wait of its own, which would be for the end of the
@@ -112,26 +133,6 @@ __device__ __forceinline__ bool plan_fits(const AttendArgs& a, const AttendHead&
   if (!fits && threadIdx.x == 0) note_error(a.g.err, ASL_ERR_WORKSPACE, -1);
   return fits;
 }
-// A group's tiles, chunks and cost.  All chunks but the last have as many tokens as fit (and more than 128 rows).
-struct WideShape {
-  int tiles, whole, rest, chunks, stripe, stripes;
-  int sum;                                 // cost of one tile of every chunk
-  __device__ __forceinline__ WideShape(int ntok, int pfx, int G, int stripe_) {
-    const int T = wide_tokens(G);
-    tiles = (pfx + WIDE_KEYS - 1) / WIDE_KEYS;
-    whole = ntok / T;
-    rest = ntok - whole * T;
-    chunks = whole + (rest > 0);
-    sum = 2 * whole + (rest ? weight_of(rest, G) : 0);
-    stripe = chunks > 1 ? stripe_ : tiles;
-    stripes = tiles ? (tiles + stripe - 1) / stripe : 0;
-  }
-  static __device__ __forceinline__ int weight_of(int tokens, int G) { return tokens * G > WIDE_ROWS / 2 ? 2 : 1; }
-  __device__ __forceinline__ int weight(int chunk, int G) const { return chunk < whole ? 2 : weight_of(rest, G); }
-  __device__ __forceinline__ int tiles_of(int s) const { return min(stripe, tiles - s * stripe); }
-  // cost before a chunk of a stripe
-  __device__ __forceinline__ int before(int s, int chunk) const { return s * stripe * sum + tiles_of(s) * 2 * chunk; }
-};
 __device__ __forceinline__ AttendStart load_start(const AttendStart* s) {
   AttendStart r;
 #pragma unroll
