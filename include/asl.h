@@ -449,6 +449,8 @@ asl_status asl_pages_status(asl_ctx* ctx, const asl_pages* pages, void* stream, 
  * the stream, so that no other thread may launch on it meanwhile.  The workspace (asl_attend_workspace bytes, 256-byte
  * aligned) carries the plan and the parts of rows whose keys are split over several blocks; calls that share it have to be
  * ordered one behind another.
+ * Tokens of one sequence share nothing with one another: they go 16 rows (token, query head of a kv head) at a time, each reading
+ * the sequence's keys; the time of hundreds of tokens of one sequence on a long prompt grows with their number.
  * H_q is a multiple of H_k with H_q / H_k <= 128.  An asl_attend whose workspace holds no plan for its cache and its sizes writes
  * nothing and notes ASL_ERR_WORKSPACE (the first bytes of the plan say what it is for: zero 256 of a workspace that may hold old
  * ones).  Where the table names a page that the pool does not have, page 0 is read in its place and ASL_ERR_INVALID noted with the

@@ -10,10 +10,10 @@
 // way by four more warps.  A prefix is a multiple of the page size, so tiles need no masks; a last tile of fewer keys makes
 // fewer products.
 //
-// What bounds it: a tile of 256 rows is 32 products of 64 clk; the kernel takes about 3500 clk for it, most of the rest a stream's
-// round from S to its weights and back, and power: kept up, the large cases run at 1000 W and 1.5 to 1.7 GHz (1040 rows on 64K
-// tokens, 8 kv heads: 270 us, 1.0 PFLOP/s; 192 rows on 128K tokens: 116 us, 4.6 TB/s), where schedules of fewer clocks have run at
-// lower ones.  With up to 128 rows HBM's latency counts: 4 TB/s of 8K prompts.
+// What bounds it: a tile of 256 rows is 32 products of 64 clk; the kernel takes about 3500 clk for it (2.0 us; E4M3 keys 2.4) and 17 us
+// for its two ends, most of the rest a stream's round from S to its weights and back, and power: kept up, the large cases run at 1000 W
+// and 1.5 to 1.7 GHz (1040 rows on 64K tokens, 8 kv heads: 294 us, 0.95 PFLOP/s; 192 rows on 128K tokens: 130 us, 4.1 TB/s), where
+// schedules of fewer clocks have run at lower ones.  With up to 128 rows HBM's latency counts: 4 TB/s of 8K prompts.
 #include "asl_ptx.cuh"
 #include "attend.cuh"
 
