@@ -555,6 +555,15 @@ class Batch:
             self.workspace = cache.torch.empty(self.ws_bytes, dtype=cache.torch.uint8, device=cache.dev)
             self.workspace[:256].zero_()               # no plan that an earlier owner of the memory left there
             self.ws = self.workspace.data_ptr()
+        self.torch, self.streams = cache.torch, {_current_stream()}
+
+    def used_on(self, stream: int) -> None:
+        """The calls run on a stream that is not the tensors' own: their memory is not to be given to others before that stream is
+        through with them."""
+        self.streams.add(stream)
+        for x in (self.workspace, self.slots, self.cu_q):
+            if x is not None:
+                x.record_stream(self.torch.cuda.current_stream())
 
 
 class PagedCache:
@@ -644,10 +653,14 @@ class PagedCache:
             got = self._strides[key] = (C.c_int64 * 2)(*key)
         return got
 
-    def _here(self, batch: Batch):
+    def _stream_of(self, batch: Batch) -> int:
+        """The current stream, for a call on the batch."""
         if batch.device != self._device:
             raise AslError(ASL_ERR_INVALID, "batch: of a cache on another device")
-        return batch.ref
+        stream = _current_stream()
+        if stream not in batch.streams:
+            batch.used_on(stream)
+        return stream
 
     def batch(self, slots, cu_q, n_tokens: int, n_q_heads: Optional[int] = None) -> Batch:
         """Sequences of a step: entry i is slot ``slots[i]`` (-1: padding) and owns tokens ``cu_q[i]`` .. ``cu_q[i+1]``, its last ones
@@ -688,15 +701,17 @@ class PagedCache:
         """K and V rows [n_tokens][H_k][d] of the batch's tokens, to the ends of their sequences."""
         ks = self._rows(k_new, "k_new", batch.n_tokens, self.pages.n_kv_heads, self._k_type is not self._bf16)
         vs = self._rows(v_new, "v_new", batch.n_tokens, self.pages.n_kv_heads)
-        _check(_lib.asl_pages_append(self.ctx, self._ref, layer, self._here(batch), k_new.data_ptr(), v_new.data_ptr(), ks, vs,
-                                     _current_stream()), "asl_pages_append")
+        stream = self._stream_of(batch)
+        _check(_lib.asl_pages_append(self.ctx, self._ref, layer, batch.ref, k_new.data_ptr(), v_new.data_ptr(), ks, vs, stream),
+               "asl_pages_append")
 
     def plan(self, batch: Batch, share: int = 1) -> None:
         """Deals out the attention of the step; again whenever lengths, pages or the batch have changed.  Prefixes that neighbours
         share are read once for all of them with ``share`` 1 where that saves enough, 2 wherever there are any, 0 nowhere."""
         batch.share = int(share)
-        _check(_lib.asl_attend_plan(self.ctx, self._ref, self._here(batch), batch.n_q_heads or 0, batch.share, batch.ws, batch.ws_bytes,
-                                    _current_stream()), "asl_attend_plan")
+        stream = self._stream_of(batch)
+        _check(_lib.asl_attend_plan(self.ctx, self._ref, batch.ref, batch.n_q_heads or 0, batch.share, batch.ws, batch.ws_bytes, stream),
+               "asl_attend_plan")
 
     def attend(self, layer: int, batch: Batch, q, out=None, lse=None):
         """Attention of the batch's tokens, q [n_tokens][H_q][d] bf16, over their sequences; out likewise (dense), lse
@@ -709,8 +724,9 @@ class PagedCache:
             raise AslError(ASL_ERR_INVALID, "out: dense [n_tokens][H_q][d] bf16")
         if lse is not None and (not lse.is_contiguous() or lse.numel() < n * heads or lse.dtype is not self._f32 or lse.get_device() != self._device):
             raise AslError(ASL_ERR_INVALID, "lse: dense [n_tokens][H_q] fp32")
-        _check(_lib.asl_attend(self.ctx, self._ref, layer, self._here(batch), heads, batch.share, q.data_ptr(), strides, out.data_ptr(),
-                               0 if lse is None else lse.data_ptr(), batch.ws, batch.ws_bytes, _current_stream()), "asl_attend")
+        stream = self._stream_of(batch)
+        _check(_lib.asl_attend(self.ctx, self._ref, layer, batch.ref, heads, batch.share, q.data_ptr(), strides, out.data_ptr(),
+                               0 if lse is None else lse.data_ptr(), batch.ws, batch.ws_bytes, stream), "asl_attend")
         return out
 
     def check(self) -> None:

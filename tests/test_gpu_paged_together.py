@@ -96,3 +96,39 @@ def test_tokens_before_their_sequences_beginning(page, fp8):
     cu = np.concatenate([[0], np.cumsum(counts)]).tolist()
     for share in (0, 2):
         check_attention(both, 0, slots, cu, 8, share=share)
+
+
+def spoil(n_bytes, count):
+    """Takes as much of the allocator's memory as `count` tensors of that size and fills it."""
+    return [torch.full((n_bytes,), 0xff, dtype=torch.uint8, device="cuda") for _ in range(count)]
+
+
+def test_a_batch_dropped_while_another_stream_is_at_work():
+    """The batch belongs to one stream's memory and is used on another: what it held is not given away before that one has read it."""
+    both = Both(kv_heads=2, page=16, n_pages=60, max_seqs=6, max_pages=12, seed=5)
+    both.fill([100, 30, 64, 1, 17, 90])
+    c, q = both.cache, queries(both.rng, 6, 8)
+    k, v = [both.dev(x) for x in both.new_rows(6, 2, 128)]
+    batch = c.batch(ints(range(6)), ints(range(7)), n_tokens=6, n_q_heads=8)
+    c.append(0, batch, k, v)
+    c.plan(batch)
+    right = c.attend(0, batch, q[0])
+    c.check()
+    page, side = int(both.oracle.table[0, 99 // 16]), torch.cuda.Stream()
+    for _ in range(3):
+        batch = c.batch(ints(range(6)), ints(range(7)), n_tokens=6, n_q_heads=8)
+        c.k[0, page, :, 99 % 16] = 0
+        torch.cuda.synchronize()
+        size = batch.ws_bytes
+        with torch.cuda.stream(side):
+            c.plan(batch)
+            torch.cuda._sleep(200_000_000)
+            c.append(0, batch, k, v)
+            out = c.attend(0, batch, q[0])
+        del batch
+        held = spoil(size, 1) + spoil(64, 3000)
+        torch.cuda.synchronize()
+        c.check()
+        del held
+        assert torch.equal(c.k[0, page, :, 99 % 16].view(torch.int16), k[0].view(torch.int16))
+        assert torch.equal(out, right)

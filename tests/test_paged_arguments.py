@@ -18,6 +18,7 @@ def bare(codes=False):
 def a_batch(n_tokens=2, n_q_heads=4):
     b = object.__new__(B.Batch)
     b.n_tokens, b.n_q_heads, b.share, b.ws, b.ws_bytes, b.ref, b.device = n_tokens, n_q_heads, 1, 0, 0, None, -1
+    b.streams = set()
     return b
 
 
