@@ -426,6 +426,8 @@ class LayerPath:
         if cache.dev != self.dev or slots is None or slots.numel() != self.batch:
             raise AslError(ASL_ERR_INVALID, "store_into: a cache on the path's device, one slot per request")
         self._pages = (cache, cache._ints(slots, "slots"))
+        if slots.is_cuda:
+            slots.record_stream(self.side2)             # where they are read, perhaps when the path has been given others
 
     def set_controller(self, mode: int) -> None:
         """ASL_CONTROLLER_LATCH: selections are final on the device and ``run_layer`` tells the library the

@@ -132,3 +132,36 @@ def test_a_batch_dropped_while_another_stream_is_at_work():
         del held
         assert torch.equal(c.k[0, page, :, 99 % 16].view(torch.int16), k[0].view(torch.int16))
         assert torch.equal(out, right)
+
+
+def test_slots_replaced_while_a_layer_is_stored():
+    """store_into's slots are read on a side stream, which may be behind when the path is given others."""
+    wl = I.workload("C3", n_q_heads=8, n_kv_heads=2, window=32, seqlens=(100, 200), budgets=(64, 64), layers=1, l_min=1, l_obs=2)
+    x = I.layer_inputs(wl, 0, seed=3)
+    path, dense = make_path(wl), make_path(wl)
+    args = [to_dev(x[n]) for n in ("q_obs", "k", "v")]
+    dense.run_layer(*args, 0)
+    dense.join()
+    cache = B.PagedCache(page_size=64, n_kv_heads=2, n_pages=4, max_seqs=2, max_pages=2)
+    cache.reserve(ints([64, 64]))
+    path.run_layer(*args, 0)
+    path.join()
+    path.reset()
+    for _ in range(3):
+        cache.k.zero_()
+        path.store_into(cache, ints([1, 0]))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(path.side2):
+            torch.cuda._sleep(200_000_000)
+        path.run_layer(*args, 0)
+        path.store_into(None)
+        held = spoil(8, 3000)
+        path.join()
+        torch.cuda.synchronize()
+        cache.check()
+        del held
+        for b, slot in ((0, 1), (1, 0)):
+            got = cache.k[0, int(cache.table[slot, 0])]
+            assert torch.equal(got.view(torch.int16), dense.k_out[:, 64 * b:64 * b + 64].view(torch.int16))
+        path.reset()
+    path.close(), dense.close()
