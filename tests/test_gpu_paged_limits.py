@@ -158,3 +158,65 @@ def test_how_many_pages_are_missing(slots, each):
     missing = min(slots * each - 4 + 2 - 48, 2 ** 31 - 1)
     assert B.asl_pages_status(cache.ctx, cache.pages) == (B.ASL_ERR_PAGES, missing)
     assert length[:3].tolist() == [20, 20, 0] and refs.sum().item() == 4
+
+
+def test_the_smallest_cache():
+    """One page, one slot, one head: every call, up to the page's end and over it."""
+    both = Both(kv_heads=1, page=16, n_pages=1, max_seqs=1, max_pages=1)
+    both.fill([1])
+    check_attention(both, 0, [0], [0, 1], 1, share=2)
+    both.fill([16])
+    check_attention(both, 0, [0], [0, 16], 1, share=1)
+    both.cache.reserve(ints([17]))
+    assert B.asl_pages_status(both.cache.ctx, both.cache.pages) == (B.ASL_ERR_INVALID, 0)
+    both.trim([15])
+    both.same_books()
+    check_attention(both, 0, [0], [0, 2], 3, share=2)
+    both.trim([0])
+    both.same_books()
+    check_attention(both, 0, [0], [0, 1], 1, share=2)
+
+
+@pytest.mark.parametrize("kv_heads,group,page,fp8", [(300, 1, 16, False), (257, 3, 16, True), (40, 128, 32, False)])
+def test_many_heads(kv_heads, group, page, fp8):
+    both = Both(kv_heads=kv_heads, page=page, n_pages=30, max_seqs=6, max_pages=10, layers=2, fp8=fp8, seed=1)
+    both.fill([150, 0, 0, 0, 5, 0])
+    both.fork([-1, 0, 0, 0, -1, -1])
+    both.fill([-1, 151, 155, 152, -1, -1])
+    both.reserve([-1] * 5 + [9])
+    for share in (0, 2):
+        check_attention(both, 1, [1, 2, 3, 4], [0, 1, 3, 4, 5], kv_heads * group, share=share)
+    idx = np.stack([np.sort(both.rng.choice(150, 9, replace=False)) for _ in range(kv_heads)])
+    both.cache.compact(1, ints([0]), ints([5]), ints([0, 9]), torch.from_numpy(idx.astype(np.int32)).cuda(), max_kept=9)
+    for h in range(kv_heads):
+        k, v = both.oracle.rows(both.oracle.k, 1, 0, h).copy(), both.oracle.rows(both.oracle.v, 1, 0, h).copy()
+        for r in range(9):
+            both.oracle.put(1, 5, r, h, k[idx[h, r]], v[idx[h, r]])
+    both.cache.check()
+    both.same_rows()
+    both.same_books()
+
+
+def test_as_many_slots_as_a_cache_has():
+    """65536 slots: the last ones and some between grow, fork, are cut and freed."""
+    n = 65536
+    both = Both(kv_heads=1, page=16, n_pages=3000, max_seqs=n, max_pages=5, seed=1)
+    some = [0, 1023, 1024, 30000, n - 2]
+    want = [-1] * n
+    for i, s in enumerate(some):
+        want[s] = 20 + i
+    both.fill(want)
+    parent = [-1] * n
+    for i in range(1000):
+        parent[40000 + i] = some[i % 5]
+    parent[n - 1] = n - 2
+    both.fork(parent)
+    want = [-1] * n
+    for i in list(range(40000, 41000)) + [n - 1]:
+        want[i] = 40
+    both.reserve(want)
+    both.same_books()
+    both.same_rows()
+    both.trim([0 if i % 3 else -1 for i in range(n)])
+    both.same_books()
+    both.cache.check()
